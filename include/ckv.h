@@ -51,7 +51,8 @@ enum {
   CKV_EWORKSPACE = -5  /* workspace too small or misaligned */
 };
 
-enum { CKV_BF16 = 1, CKV_F32 = 2 };                 /* out_dtype */
+enum { CKV_BF16 = 1, CKV_F32 = 2,                    /* out_dtype */
+       CKV_E4M3 = 3 };                               /* ckv_pages.dtype: CKV_BF16 or CKV_E4M3 */
 enum { CKV_REWARD_TOPP_HIT = 0,                      /* Alg. 1: reward 1 for entries in the top-p hit set */
        CKV_REWARD_ATTN_WEIGHTED = 1 };               /* variant: reward = mean attention weight, every entry stored */
 enum { CKV_FLAG_HIT = 1,                             /* per-slot flag as exported: entry was in the last step's hit set */
@@ -345,7 +346,125 @@ int ckv_join(ckv_ctx* ctx, void* stream);
  * for calibrating profiler byte counters.  Pointers 16-byte aligned. */
 int ckv_bandwidth_probe(const void* src, void* dst, size_t bytes, void* sink, void* stream);
 
+/* ---- A cache in pages ------------------------------------------------------
+ * Beside the budgeted caches of a context: whole caches, which evict nothing, in
+ * pages of page_size entries that a table of page numbers hands to sequences.
+ * They spend less in the two ways that do not evict: rows in 8 bits (a row is
+ * the 128 values of one key or value), and attention that reads only the pages
+ * that a bound on their logits picks for each query.  ckv_paged_read gives rows
+ * back in bf16, for ckv_load_prompt for instance.
+ *
+ * These calls have no context and keep nothing between calls: pools, table,
+ * lengths and workspace are the caller's device memory, and no call waits or
+ * allocates, so all of them can be captured into a graph (lengths and table are
+ * read when it is replayed; the workspace then belongs to the graph).  Calls
+ * that run at the same time need workspaces of their own.  The current device
+ * must be the one that holds the buffers and the stream.  ckv_last_error(NULL)
+ * says what the thread's last refused call complained about.
+ *
+ * Device memory holds what the host cannot check; kernels check it instead, do
+ * without what is wrong and OR a bit into *status (if status is not NULL; the
+ * library never clears it): */
+enum { CKV_PAGED_BAD_PAGE = 1,    /* a table entry that a sequence needs is not in [0, n_pages): its rows are neither read nor written */
+       CKV_PAGED_BAD_LENGTH = 2,  /* a length outside [0, max_length] (taken as the nearer of these), or rows that do not fit it (left out) */
+       CKV_PAGED_BAD_PICK = 4 };  /* a picked page that the sequence does not have (left out) */
+
+/* The pools of one layer.  k, v: dev [n_pages][n_kv_heads][page_size][128] with
+ * the strides given, in elements (multiples of 16 bytes; a page may for instance
+ * hold a slot's heads side by side), 16-byte aligned, rows contiguous.
+ *   CKV_BF16: the values as they are; scales unused (NULL).
+ *   CKV_E4M3: codes, and one power of two per row: scales dev
+ *     [n_pages][n_kv_heads][page_size][2] uint8 (key, value; strides in bytes,
+ *     multiples of 8; 8-byte aligned) holds E + 127, where E is the smallest
+ *     integer in [-100, 120] for which the row's largest finite magnitude is at
+ *     most 448 * 2^E.  A code is x / 2^E, exact, rounded to the nearest e4m3 (ties
+ *     to even; no number and infinities become the format's NaN); code * 2^E is
+ *     a bf16 number (infinite where magnitudes from 3.3e38 on round up).  Caches that a caller fills need E in that range.
+ *   bounds: dev bf16 [n_pages][n_kv_heads][2][128], or NULL: least and largest key
+ *     value of each dimension over the page's rows (NaN left out), kept by
+ *     ckv_paged_append and read by ckv_paged_select; strides in elements,
+ *     multiples of 8, 16-byte aligned.
+ * page_size: 16, 32, 64, 128 or 256.  head_dim: 128. */
+typedef struct {
+  int32_t n_pages, page_size, n_kv_heads, head_dim, dtype;
+  int64_t page_stride, head_stride, slot_stride;
+  int64_t scale_page_stride, scale_head_stride;
+  int64_t bounds_page_stride, bounds_head_stride;
+  void* k;
+  void* v;
+  uint8_t* scales;
+  void* bounds;
+  int32_t* status;        /* dev, or NULL */
+} ckv_pages;
+
+/* The sequences of a call.  table: dev [batch][columns], rows table_stride
+ * elements apart: column c of row b is the pool page of the sequence's positions
+ * c * page_size .. (c + 1) * page_size - 1.  Entries behind a sequence's end are
+ * not looked at.  Sequences may share pages that nobody writes.  lengths: dev
+ * [batch], entries of each sequence, in all calls of a step those of the step's
+ * new rows included.  max_length <= columns * page_size: the most that a length
+ * may be; launches and workspace are sized by it. */
+typedef struct {
+  const int32_t* table;
+  const int32_t* lengths;
+  int64_t table_stride;
+  int32_t batch, columns, max_length;
+} ckv_seqs;
+
+/* Rows in bf16 that a call writes into the cache or reads from it: of sequence b the positions first[b] .. (first: dev [batch];
+ * NULL: lengths[b] - rows, or 0 if that is negative) up to lengths[b] - 1, at most `rows` of them.  Row i of sequence b and KV head h
+ * lies at b * seq_stride + i * row_stride + h * head_stride (in elements, multiples of 8), or, with starts (dev [batch + 1]:
+ * sequences packed one after another), at (starts[b] + i) * row_stride + h * head_stride, and then there are at most
+ * starts[b + 1] - starts[b] of them; `total` is the number of rows that k and v hold.  k, v 16-byte aligned.  Rows behind a
+ * sequence's last are not touched. */
+typedef struct {
+  void* k;
+  void* v;
+  const int32_t* first;
+  const int32_t* starts;
+  int64_t seq_stride, row_stride, head_stride;
+  int32_t rows, total;
+} ckv_rows;
+
+/* Queries of one new token per sequence: dev bf16, head g of sequence b at b * seq_stride + g * head_stride (in elements, multiples
+ * of 8, 16-byte aligned).  n_q_heads = G * n_kv_heads with G <= 16. */
+typedef struct {
+  const void* q;
+  int64_t seq_stride, head_stride;
+  int32_t n_q_heads;
+} ckv_query;
+
+/* Writes rows into their pages and brings the pages' bounds up to date (those of a page whose first slot is written start anew; writing a
+ * position again leaves bounds that still hold, if wider than need be).  No two rows of a call may go to the same place: sequences of one call
+ * must not share pages that it writes. */
+int ckv_paged_append(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_rows* rows, void* stream);
+
+/* Reads rows back as bf16 (exact: see ckv_pages). */
+int ckv_paged_read(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_rows* rows, void* stream);
+
+/* Bytes of workspace that ckv_paged_attend (n_picked pages per KV head, 0: all entries) and ckv_paged_select need for these sizes on the
+ * current device; it depends on max_length and the sizes alone.  0 if they are refused. */
+size_t ckv_paged_workspace_bytes(const ckv_pages* pages, const ckv_seqs* seqs, int32_t n_q_heads, int32_t n_picked);
+
+/* Attention of one new token per sequence (whose own row has been appended): out[b][g] = softmax(softmax_scale q K^T) V over the sequence's
+ * entries, out dev out_dtype [batch][n_q_heads][128]; lse (dev float [batch][n_q_heads], or NULL) the natural logarithm of the sum of the
+ * exponentials, with which partial attentions can be joined.  A sequence without entries gets zeros and -inf; so does a head all of whose
+ * logits are -inf.  With `picked` (dev [batch][n_kv_heads][n_picked], as ckv_paged_select leaves it) only the entries of the listed pages of the
+ * sequence take part; -1 stands for no page, the order does not matter, and a page listed twice counts twice.  workspace: 256-byte aligned, not needed where
+ * ckv_paged_workspace_bytes says 256.  Values of entries in use must be finite. */
+int ckv_paged_attend(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_query* query, float softmax_scale, const int32_t* picked,
+                     int32_t n_picked, void* out, int32_t out_dtype, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Picks `keep` pages of each sequence and KV head for a token: the keep_first first and keep_last last ones (attention sinks, the latest
+ * entries), and of the others those with the highest scores, where a page's score is the sum over the KV head's query heads of the largest q.k
+ * that its bounds allow, sum_d max(q_d least_d, q_d largest_d), added up in 64 bits and rounded once to float (a zero of q adds nothing, whatever the bounds; no number
+ * counts as highest; ties: the lowest page).  picked: dev [batch][n_kv_heads][keep], ascending, -1 behind the last if a sequence has fewer pages.  Sequences of up to
+ * 32768 pages (by max_length). */
+int ckv_paged_select(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_query* query, int32_t keep, int32_t keep_first, int32_t keep_last,
+                     int32_t* picked, void* workspace, size_t workspace_bytes, void* stream);
+
 const char* ckv_strerror(int code);
+/* Detail of the context's last error; NULL: of the calling thread's last refused or failed ckv_paged_* call. */
 const char* ckv_last_error(const ckv_ctx* ctx);
 
 #ifdef __cplusplus

@@ -15,12 +15,13 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libckv.so")
 
 OK, EINVAL, ECAPACITY, ESTATE, EHIP, EWORKSPACE = 0, -1, -2, -3, -4, -5
-BF16, F32 = 1, 2
+BF16, F32, E4M3 = 1, 2, 3
 REWARD_TOPP_HIT, REWARD_ATTN_WEIGHTED = 0, 1
 FLAG_HIT, FLAG_SLIP = 1, 2
 FUSE_EVICT = 1
 ATTENTION_ONLY = 2
 DEFER_BOOKKEEPING = 4
+BAD_PAGE, BAD_LENGTH, BAD_PICK = 1, 2, 4          # PagedCache.status
 
 EXPORTS = [
     "ckv_workspace_bytes", "ckv_init", "ckv_destroy", "ckv_load_prompt", "ckv_seed_prompt", "ckv_load_cache", "ckv_decode_step",
@@ -29,6 +30,7 @@ EXPORTS = [
     "ckv_rebudget", "ckv_rebalance", "ckv_pool_slots", "ckv_probe", "ckv_probe_noalloc", "ckv_get_budgets", "ckv_get_lengths", "ckv_get_segments", "ckv_set_budgets", "ckv_get_time",
     "ckv_set_time", "ckv_status", "ckv_export_unit", "ckv_import_unit", "ckv_profile_enable",
     "ckv_profile_read", "ckv_set_path", "ckv_path_info", "ckv_join", "ckv_bandwidth_probe", "ckv_strerror", "ckv_last_error",
+    "ckv_paged_append", "ckv_paged_read", "ckv_paged_workspace_bytes", "ckv_paged_attend", "ckv_paged_select",
 ]
 
 
@@ -48,6 +50,29 @@ class Buffers(C.Structure):
     _fields_ = [("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("crf", C.c_void_p), ("tau", C.c_void_p),
                 ("pos", C.c_void_p), ("flags", C.c_void_p), ("workspace", C.c_void_p),
                 ("workspace_bytes", C.c_size_t)]
+
+
+class Pages(C.Structure):
+    _fields_ = [("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+                ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("slot_stride", C.c_int64),
+                ("scale_page_stride", C.c_int64), ("scale_head_stride", C.c_int64),
+                ("bounds_page_stride", C.c_int64), ("bounds_head_stride", C.c_int64),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("scales", C.c_void_p), ("bounds", C.c_void_p), ("status", C.c_void_p)]
+
+
+class Seqs(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("lengths", C.c_void_p), ("table_stride", C.c_int64),
+                ("batch", C.c_int32), ("columns", C.c_int32), ("max_length", C.c_int32)]
+
+
+class Rows(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("first", C.c_void_p), ("starts", C.c_void_p),
+                ("seq_stride", C.c_int64), ("row_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("rows", C.c_int32), ("total", C.c_int32)]
+
+
+class Query(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("seq_stride", C.c_int64), ("head_stride", C.c_int64), ("n_q_heads", C.c_int32)]
 
 
 _lib = None
@@ -96,6 +121,12 @@ def load():
     lib.ckv_path_info.argtypes = [vp, C.POINTER(i32), C.POINTER(i32)]
     lib.ckv_join.argtypes = [vp, vp]
     lib.ckv_bandwidth_probe.argtypes = [vp, vp, C.c_size_t, vp, vp]
+    lib.ckv_paged_append.argtypes = [vp, vp, vp, vp]
+    lib.ckv_paged_read.argtypes = [vp, vp, vp, vp]
+    lib.ckv_paged_workspace_bytes.restype = C.c_size_t
+    lib.ckv_paged_workspace_bytes.argtypes = [vp, vp, i32, i32]
+    lib.ckv_paged_attend.argtypes = [vp, vp, vp, C.c_float, vp, i32, vp, i32, vp, vp, C.c_size_t, vp]
+    lib.ckv_paged_select.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, C.c_size_t, vp]
     lib.ckv_strerror.restype = C.c_char_p
     lib.ckv_strerror.argtypes = [C.c_int]
     lib.ckv_last_error.restype = C.c_char_p
@@ -431,6 +462,212 @@ class CrystalKV:
         ms, n = C.c_double(0.0), C.c_int32(0)
         self._check(self.lib.ckv_profile_read(self.ctx, C.byref(ms), C.byref(n)))
         return ms.value, n.value
+
+
+class PagedSequences:
+    """A table and lengths on the device, as PagedCache.sequences checked them, for that cache and others on its device (a model's layers).  Both are
+    read by the kernels of each call, so they may change between calls."""
+
+    def __init__(self, cache, table, lengths, max_length):
+        t = cache.torch
+        if table.dtype != t.int32 or table.dim() != 2 or lengths.dtype != t.int32 or lengths.shape != table.shape[:1]:
+            raise CkvError(EINVAL, "table must be int32 [batch][columns] and lengths int32 [batch]")
+        if table.numel() == 0 or (table.shape[1] > 1 and table.stride(1) != 1) or not lengths.is_contiguous():
+            raise CkvError(EINVAL, "table needs a sequence, a column and contiguous rows, lengths must be contiguous")
+        cache._same_device(table, lengths)
+        self.batch, self.columns = table.shape
+        self.max_length = int(max_length) if max_length is not None else self.columns * cache.page_size
+        self.table, self.lengths = table, lengths
+        self._struct = Seqs(table.data_ptr(), lengths.data_ptr(), _stride(table, 0, self.columns), self.batch, self.columns, self.max_length)
+        self._ref = C.addressof(self._struct)
+        self._workspace = {}
+
+
+def _stride(x, dim, unit):
+    """A dimension's stride; any will do where it has one element."""
+    return x.stride(dim) if x.shape[dim] > 1 else unit
+
+
+class PagedCache:
+    """The pools of a cache in pages (one layer's), over torch tensors: ckv_paged_append, _read, _attend and _select of include/ckv.h.
+
+    k, v: [n_pages][n_kv_heads][page_size][128], bf16 or float8_e4m3fn, any strides that are multiples of 16 bytes (a pool that keeps a slot's
+    heads side by side is passed as its view); scales: uint8 [n_pages][n_kv_heads][page_size][2], with float8_e4m3fn; bounds: bf16
+    [n_pages][n_kv_heads][2][128], needed by select and kept by append if it is there.  Calls enqueue on the current stream
+    of the pools' device; workspaces come from torch's allocator, call by call."""
+
+    def __init__(self, k, v, *, scales=None, bounds=None):
+        import torch
+        self.torch = torch
+        self.lib = load()
+        if k.dim() != 4 or k.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+            raise CkvError(EINVAL, "k must be bf16 or float8_e4m3fn [n_pages][n_kv_heads][page_size][128]")
+        if v.dtype != k.dtype or v.shape != k.shape or v.stride() != k.stride() or k.stride(3) != 1:
+            raise CkvError(EINVAL, "k and v must be alike, with contiguous rows")
+        self.k, self.v, self.scales, self.bounds, self.device = k, v, scales, bounds, k.device
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        self.dtype = BF16 if k.dtype == torch.bfloat16 else E4M3
+        if (scales is None) != (self.dtype == BF16):
+            raise CkvError(EINVAL, "scales belong to a float8_e4m3fn cache, and to no other")
+        s = b = (0, 0)
+        if scales is not None:
+            if scales.dtype != torch.uint8 or scales.shape != (*k.shape[:3], 2) or scales.stride()[2:] != (2, 1):
+                raise CkvError(EINVAL, "scales must be uint8 [n_pages][n_kv_heads][page_size][2], contiguous within a page and head")
+            s = (_stride(scales, 0, 2 * self.page_size), _stride(scales, 1, 2 * self.page_size))
+        if bounds is not None:
+            if bounds.dtype != torch.bfloat16 or bounds.shape != (*k.shape[:2], 2, self.head_dim) or bounds.stride()[2:] != (self.head_dim, 1):
+                raise CkvError(EINVAL, "bounds must be bf16 [n_pages][n_kv_heads][2][128], contiguous within a page and head")
+            b = (_stride(bounds, 0, 256), _stride(bounds, 1, 256))
+        self._same_device(v, scales, bounds)
+        if self.device.type != "cuda":
+            raise CkvError(EINVAL, f"the pools must be device memory, not on {self.device}")
+        self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._index = self.device.index if self.device.index is not None else 0
+        self._struct = Pages(self.n_pages, self.page_size, self.n_kv_heads, self.head_dim, self.dtype, _stride(k, 0, self.head_dim), _stride(k, 1, self.head_dim),
+                             k.stride(2), *s, *b, k.data_ptr(), v.data_ptr(), scales.data_ptr() if scales is not None else None,
+                             bounds.data_ptr() if bounds is not None else None, self._status.data_ptr())
+        self._ref = C.addressof(self._struct)
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self._scale = 1.0 / float(np.sqrt(self.head_dim))
+
+    @classmethod
+    def empty(cls, n_pages, page_size, n_kv_heads, *, dtype=E4M3, bounds=False, device="cuda:0"):
+        """A cache of its own pools, nothing in them yet."""
+        import torch
+        if dtype not in (BF16, E4M3):
+            raise CkvError(EINVAL, "dtype must be BF16 or E4M3")
+        k, v = (torch.empty((n_pages, n_kv_heads, page_size, 128), dtype=torch.bfloat16 if dtype == BF16 else torch.float8_e4m3fn, device=device) for _ in range(2))
+        return cls(k, v, scales=None if dtype == BF16 else torch.empty((n_pages, n_kv_heads, page_size, 2), dtype=torch.uint8, device=device),
+                   bounds=torch.empty((n_pages, n_kv_heads, 2, 128), dtype=torch.bfloat16, device=device) if bounds else None)
+
+    # ------------------------------------------------------------------ plumbing
+    def _same_device(self, *tensors):
+        for x in tensors:
+            if x is not None and x.device != self.device:
+                raise CkvError(EINVAL, f"a tensor on {x.device} with a cache on {self.device}")
+
+    def _call(self, entry, *args):
+        """entry(*args, stream) on the pools' device."""
+        cuda = self.torch.cuda
+        if self._raw_stream is not None and cuda.current_device() == self._index:
+            rc = entry(*args, self._raw_stream(self._index))
+        else:
+            with cuda.device(self.device):
+                rc = entry(*args, cuda.current_stream(self.device).cuda_stream)
+        if rc != OK:
+            raise CkvError(rc, self.lib.ckv_last_error(None).decode())
+
+    def _workspace(self, seqs, n_q_heads, n_picked, least=256):
+        key = (n_q_heads, n_picked, self.n_kv_heads, self.page_size, self.bounds is None)
+        n = seqs._workspace.get(key)
+        if n is None:
+            with self.torch.cuda.device(self.device):
+                n = self.lib.ckv_paged_workspace_bytes(self._ref, seqs._ref, n_q_heads, n_picked)
+            if n == 0:
+                raise CkvError(EINVAL, self.lib.ckv_last_error(None).decode())
+            seqs._workspace[key] = n
+        return self.torch.empty(n, dtype=self.torch.uint8, device=self.device) if n > least else None, n
+
+    def _rows(self, seqs, k, v, rows, first, starts):
+        t = self.torch
+        for x in (k, v):
+            if x.dtype != t.bfloat16 or x.shape != k.shape or x.stride() != k.stride() or x.stride(-1) != 1:
+                raise CkvError(EINVAL, "rows must be two alike bf16 tensors with contiguous rows")
+        self._same_device(k, v, first, starts)
+        for x, n in ((first, seqs.batch), (starts, seqs.batch + 1)):
+            if x is not None and (x.dtype != t.int32 or x.shape != (n,) or not x.is_contiguous()):
+                raise CkvError(EINVAL, "first must be int32 [batch], starts int32 [batch + 1]")
+        packed = starts is not None
+        if packed and rows is None:
+            raise CkvError(EINVAL, "packed rows need `rows`, the most that one sequence has")
+        if not packed and k.dim() == 3:
+            k, v = k.unsqueeze(1), v.unsqueeze(1)
+        if not packed and rows is None:
+            rows = k.shape[1]
+        shape = (k.shape[0], self.n_kv_heads, self.head_dim) if packed else (seqs.batch, rows, self.n_kv_heads, self.head_dim)
+        if k.shape != shape:
+            raise CkvError(EINVAL, f"rows of shape {tuple(k.shape)}, {tuple(shape)} expected")
+        d = self.head_dim
+        return Rows(k.data_ptr(), v.data_ptr(), first.data_ptr() if first is not None else None, starts.data_ptr() if packed else None,
+                    0 if packed else _stride(k, 0, d), _stride(k, -3, d), _stride(k, -2, d), int(rows), k.shape[0] if packed else 0)
+
+    def _query(self, seqs, q):
+        if q.dtype != self.torch.bfloat16 or q.dim() != 3 or q.shape[0] != seqs.batch or q.shape[2] != self.head_dim or q.stride(2) != 1:
+            raise CkvError(EINVAL, "q must be bf16 [batch][n_q_heads][128] with contiguous rows")
+        self._same_device(q)
+        return Query(q.data_ptr(), _stride(q, 0, self.head_dim), _stride(q, 1, self.head_dim), q.shape[1])
+
+    # ------------------------------------------------------------------ calls
+    def sequences(self, table, lengths, max_length=None):
+        """What the other calls take: table int32 [batch][columns] of page numbers, lengths int32 [batch]; max_length bounds the lengths (by
+        default what the columns hold) and sizes launches and workspaces."""
+        s = PagedSequences(self, table, lengths, max_length)
+        self._workspace(s, self.n_kv_heads, 0)           # the geometry's checks
+        return s
+
+    def append(self, seqs, k, v, *, rows=None, first=None, starts=None):
+        """Writes rows: k, v bf16 [batch][rows][n_kv_heads][128] (or [batch][n_kv_heads][128], one each), or with `starts` [total][n_kv_heads][128].
+        They become positions first .. lengths - 1 of their sequences (default: the last `rows`)."""
+        r = self._rows(seqs, k, v, rows, first, starts)
+        self._call(self.lib.ckv_paged_append, self._ref, seqs._ref, C.addressof(r))
+
+    def read(self, seqs, rows, *, first=None, starts=None, total=None, out=None):
+        """The same rows back, bf16: (k, v), new tensors (uninitialised behind a sequence's last row) or `out`."""
+        t = self.torch
+        if out is None:
+            if starts is not None and total is None:
+                raise CkvError(EINVAL, "packed rows need `total` or `out`")
+            shape = (seqs.batch, int(rows)) if starts is None else (int(total),)
+            out = tuple(t.empty((*shape, self.n_kv_heads, self.head_dim), dtype=t.bfloat16, device=self.device) for _ in range(2))
+        r = self._rows(seqs, *out, rows, first, starts)
+        self._call(self.lib.ckv_paged_read, self._ref, seqs._ref, C.addressof(r))
+        return out
+
+    def attend(self, seqs, q, *, pages=None, scale=None, f32=False, lse=False, out=None):
+        """Attention of one token per sequence, q bf16 [batch][n_q_heads][128]: (out, lse), out of q's shape in bf16 or float (f32), lse float
+        [batch][n_q_heads] or None.  pages: int32 [batch][n_kv_heads][n], as select returns it: only their entries take part."""
+        t = self.torch
+        query = self._query(seqs, q)
+        n_picked = 0
+        if pages is not None:
+            if pages.dtype != t.int32 or pages.dim() != 3 or pages.shape[:2] != (seqs.batch, self.n_kv_heads) or pages.shape[2] < 1 or not pages.is_contiguous():
+                raise CkvError(EINVAL, "pages must be int32 [batch][n_kv_heads][n], n at least 1, contiguous")
+            self._same_device(pages)
+            n_picked = pages.shape[2]
+        dtype = t.float32 if f32 else t.bfloat16
+        if out is None:
+            out = t.empty(q.shape, dtype=dtype, device=self.device)
+        elif out.dtype != dtype or out.shape != q.shape or not out.is_contiguous() or out.device != self.device:
+            raise CkvError(EINVAL, f"out must be a contiguous {dtype} tensor of q's shape")
+        sums = t.empty(q.shape[:2], dtype=t.float32, device=self.device) if lse else None
+        work, n = self._workspace(seqs, q.shape[1], n_picked)
+        self._call(self.lib.ckv_paged_attend, self._ref, seqs._ref, C.addressof(query), self._scale if scale is None else scale,
+                   pages.data_ptr() if pages is not None else None, n_picked, out.data_ptr(), F32 if f32 else BF16, sums.data_ptr() if lse else None,
+                   work.data_ptr() if work is not None else None, n)
+        return out, sums
+
+    def select(self, seqs, q, keep, *, first=1, last=1, out=None):
+        """`keep` pages per sequence and KV head for q: the `first` first, the `last` last, the others by score; int32 [batch][n_kv_heads][keep], ascending,
+        -1 behind the last."""
+        t = self.torch
+        query = self._query(seqs, q)
+        shape = (seqs.batch, self.n_kv_heads, int(keep))
+        if out is None:
+            out = t.empty(shape, dtype=t.int32, device=self.device)
+        elif out.dtype != t.int32 or out.shape != shape or not out.is_contiguous() or out.device != self.device:
+            raise CkvError(EINVAL, "out must be a contiguous int32 tensor [batch][n_kv_heads][keep]")
+        work, n = self._workspace(seqs, q.shape[1], 0, 0)
+        self._call(self.lib.ckv_paged_select, self._ref, seqs._ref, C.addressof(query), int(keep), int(first), int(last), out.data_ptr(),
+                   work.data_ptr() if work is not None else None, n)
+        return out
+
+    def status(self):
+        """What kernels had to do without since the last call (BAD_PAGE, BAD_LENGTH, BAD_PICK), 0 if nothing; waits for the device."""
+        self.torch.cuda.synchronize(self.device)
+        s = int(self._status.item())
+        if s:
+            self._status.zero_()
+        return s
 
 
 def place_pools(pool_bytes, device="cuda:0", max_fraction=0.92, verbose=False, rest_bytes=0):

@@ -20,6 +20,10 @@
 #include "ckv_layer_kernel.h"
 #include "ckv_unit_kernel.h"
 
+namespace ckv {
+const char* thread_error();       // of calls without a context (ckv_paged.hip)
+}
+
 using namespace ckv;
 
 constexpr int kManyEntries = 1 << 20;   // `excess` of a layer about which the host knows nothing
@@ -1337,7 +1341,7 @@ const char* ckv_strerror(int code) {
   }
 }
 
-const char* ckv_last_error(const ckv_ctx* c) { return c ? c->err.c_str() : ""; }
+const char* ckv_last_error(const ckv_ctx* c) { return c ? c->err.c_str() : thread_error(); }
 
 
 }  // extern "C"
