@@ -36,14 +36,33 @@ CKV_PLAN RowSpan row_span(int length, int most, bool has_first, int first, bool 
   return {first, count, false};
 }
 
-// Entries per workgroup of an attention over `entries` at most for each of `units`: a power of two from 128 (a block of 32 for each of four
-// wavefronts) to what kPageSlots pages hold, the smallest that makes no more than eight workgroups per compute unit.
-CKV_PLAN int attend_piece(long long units, long long entries, int shift, int n_cu) {
-  const int most = (kPageSlots << shift) < 4096 ? kPageSlots << shift : 4096;
-  int piece = 128;
-  while (piece < most && units * ((entries + piece - 1) / piece) > 8ll * n_cu) piece *= 2;
-  return piece;
+// An attention's work in blocks of 32 entries: one for a unit (sequence, KV head) without entries, whose output somebody has to write.
+constexpr int kAttendWaves = 4;         // of a workgroup, which take blocks in turn
+CKV_PLAN int unit_blocks(int entries) { return entries > 32 ? (int)(((long long)entries + 31) / 32) : 1; }
+CKV_PLAN int unit_parts(int blocks, int share) { return blocks / share + (blocks % share != 0); }
+// The work is cut into pieces of at most an even share of all blocks, at least a block for each wavefront.
+CKV_PLAN int attend_share(int blocks, int workers) {
+  const int even = unit_parts(blocks, workers);
+  return even > kAttendWaves ? even : kAttendWaves;
 }
-CKV_PLAN int attend_pieces(long long entries, int piece) { return entries <= piece ? 1 : (int)((entries + piece - 1) / piece); }
+
+// How the host has it cut, knowing no length but the most that there can be.
+struct AttendPlan {
+  int share;            // blocks of a piece, where every unit has the same number of places for pieces; 0: workgroups look for theirs
+  int places;           // then so many for each unit
+  int workers;          // otherwise the shares of all blocks that pieces are cut by
+  long long pieces;     // workgroups
+  bool split;           // whether a unit may fall into several pieces
+};
+CKV_PLAN AttendPlan attend_plan(long long units, int entries, bool same, int n_cu) {
+  const int blocks = unit_blocks(entries), workers = 2 * n_cu;
+  if (blocks <= 3 * kAttendWaves || (blocks <= 8 * kAttendWaves && units >= n_cu)) return {blocks, 1, 0, units, false};
+  if (same || units * unit_parts(blocks, kAttendWaves) <= 4 * n_cu) {
+    const long long even = (units * blocks + workers - 1) / workers;
+    const int share = even > kAttendWaves ? (int)(even < blocks ? even : blocks) : kAttendWaves, places = unit_parts(blocks, share);
+    return {share, places, 0, units * places, places > 1};
+  }
+  return {0, 0, workers, workers + units, true};
+}
 
 }  // namespace ckv

@@ -132,19 +132,26 @@ int compute_units() {
 
 constexpr size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
-// How an attention is split, and what its pieces leave in the workspace.
+// How an attention is cut, and what its pieces leave in the workspace.
 struct Split {
-  int piece, pieces;
-  size_t partial, ml;    // bytes
+  AttendPlan plan;
+  size_t partial, ml, parts;    // bytes
+  size_t bytes() const { return partial + ml + parts; }
 };
+// Entries of a unit at most.
+long long unit_entries(const ckv_pages* p, const ckv_seqs* s, int n_picked) { return n_picked > 0 ? (long long)n_picked * p->page_size : s->max_length; }
+bool too_many(const ckv_pages* p, const ckv_seqs* s, int n_picked) {
+  return (long long)s->batch * p->n_kv_heads * unit_blocks((int)unit_entries(p, s, n_picked)) > (1ll << 30);
+}
 Split split_of(const ckv_pages* p, const ckv_seqs* s, int n_q_heads, int n_picked, int n_cu) {
-  const long long units = (long long)s->batch * p->n_kv_heads, entries = n_picked > 0 ? (long long)n_picked * p->page_size : s->max_length;
+  const long long units = (long long)s->batch * p->n_kv_heads;
   Split r{};
-  r.piece = attend_piece(units, entries, __builtin_ctz((unsigned)p->page_size), n_cu);
-  r.pieces = attend_pieces(entries, r.piece);
-  if (r.pieces > 1) {
-    r.partial = up256((size_t)s->batch * n_q_heads * r.pieces * kDim * 4);
-    r.ml = up256((size_t)s->batch * n_q_heads * r.pieces * 8);
+  r.plan = attend_plan(units, (int)unit_entries(p, s, n_picked), n_picked > 0, n_cu);
+  if (r.plan.split) {
+    const size_t G = (size_t)(n_q_heads / p->n_kv_heads);
+    r.partial = up256((size_t)r.plan.pieces * G * kDim * 4);
+    r.ml = up256((size_t)r.plan.pieces * G * 8);
+    r.parts = up256((size_t)units * 8);
   }
   return r;
 }
@@ -190,9 +197,9 @@ int ckv_paged_read(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_rows*
 size_t ckv_paged_workspace_bytes(const ckv_pages* pages, const ckv_seqs* seqs, int32_t n_q_heads, int32_t n_picked) {
   if (check(pages, seqs) != CKV_OK) return 0;
   if (n_q_heads < pages->n_kv_heads || n_q_heads % pages->n_kv_heads != 0 || n_q_heads / pages->n_kv_heads > kPagedGroup) return 0;
-  if (n_picked < 0 || (long long)n_picked * pages->page_size > kMaxLength) return 0;
+  if (n_picked < 0 || (long long)n_picked * pages->page_size > kMaxLength || too_many(pages, seqs, n_picked)) return 0;
   const Split s = split_of(pages, seqs, n_q_heads, n_picked, compute_units());
-  return std::max<size_t>(256, std::max(s.partial + s.ml, pages->bounds ? score_bytes(pages, seqs) : 0));
+  return std::max<size_t>(256, std::max(s.bytes(), pages->bounds ? score_bytes(pages, seqs) : 0));
 }
 
 int ckv_paged_attend(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_query* query, float softmax_scale, const int32_t* picked, int32_t n_picked, void* out,
@@ -204,10 +211,10 @@ int ckv_paged_attend(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_que
   if (!(softmax_scale > 0.0f) || !std::isfinite(softmax_scale)) return fail(CKV_EINVAL, "softmax_scale must be positive");
   if (picked ? n_picked < 1 : n_picked != 0) return fail(CKV_EINVAL, "n_picked must be positive with a list of pages and 0 without");
   if ((long long)n_picked * pages->page_size > kMaxLength) return fail(CKV_EINVAL, "too many pages picked");
+  if (too_many(pages, seqs, n_picked)) return fail(CKV_EINVAL, "too many entries in all (2^35)");
   const int G = query->n_q_heads / pages->n_kv_heads;
   const Split s = split_of(pages, seqs, query->n_q_heads, n_picked, compute_units());
-  if (s.pieces > kMaxGrid) return fail(CKV_EINVAL, "too many entries for pages of this size");
-  if (s.partial + s.ml > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < s.partial + s.ml)) return fail(CKV_EWORKSPACE, "workspace too small or misaligned");
+  if (s.bytes() > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < s.bytes())) return fail(CKV_EWORKSPACE, "workspace too small or misaligned");
   const Paged p = paged_of(pages, seqs);
   Attend c{};
   c.q = (const uint8_t*)query->q;
@@ -222,9 +229,11 @@ int ckv_paged_attend(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_que
   c.ml = (float*)((char*)workspace + s.partial);
   c.scale_log2e = softmax_scale * 1.44269504088896340736f;
   c.G = G;
-  c.piece = s.piece;
-  c.pieces = s.pieces;
-  const dim3 grid((unsigned)(seqs->batch * pages->n_kv_heads), (unsigned)s.pieces);
+  if (s.plan.split) c.parts = (int32_t*)((char*)workspace + s.partial + s.ml);
+  c.share = s.plan.share;
+  c.places = s.plan.places;
+  c.workers = s.plan.workers;
+  const dim3 grid((unsigned)s.plan.pieces);
   auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, (hipStream_t)stream, p, c); };
   const bool wide = G > 8, fine = out_dtype == CKV_F32;
   if (pages->dtype == CKV_E4M3) {
@@ -235,8 +244,10 @@ int ckv_paged_attend(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_que
     else fine ? launch(paged_attend_kernel<false, 3, false>) : launch(paged_attend_kernel<false, 2, false>);
   }
   if (int rc = launched("ckv_paged_attend")) return rc;
-  if (s.pieces == 1) return CKV_OK;
-  hipLaunchKernelGGL(paged_join_kernel, dim3(grid.x, (unsigned)G), dim3(kThreads), 0, (hipStream_t)stream, p, c);
+  if (!s.plan.split) return CKV_OK;
+  const unsigned units = (unsigned)(seqs->batch * pages->n_kv_heads);
+  const int heads = (int)units > compute_units() ? std::min(G, kJoinRows) : 1;
+  hipLaunchKernelGGL(paged_join_kernel, dim3(units, (unsigned)((G + heads - 1) / heads)), dim3(32 * kJoinRows), 0, (hipStream_t)stream, c, heads);
   return launched("ckv_paged_attend");
 }
 

@@ -6,6 +6,8 @@
 // powers of two a code's value is a bf16 number, so that reading back, the products' operands and a page's extremes are all exact;
 // and e4m3 loses nothing by them, since its steps are relative.
 #pragma once
+#include <type_traits>
+
 #include "ckv_lanes.h"
 #include "ckv_layout.h"
 #include "ckv_paged.h"
@@ -239,11 +241,13 @@ struct Attend {
   const int32_t* picked;     // [batch][hkv][n_picked] pages of the sequence (-1: none), or NULL
   uint8_t* out;
   float* lse;
-  float* partial;            // [unit][pieces][G][128]
-  float* ml;                 // [unit][pieces][G][2]
+  float* partial;            // [piece][G][128]
+  float* ml;                 // [piece][G][2]
+  int32_t* parts;            // [unit][2]: its first piece, and how many it has
   int64_t q_seq_stride, q_head_stride;     // bytes
   float scale_log2e;
-  int32_t G, n_picked, piece, pieces, out_bf16;
+  int32_t G, n_picked, out_bf16;
+  int32_t share, places, workers;          // AttendPlan
 };
 
 constexpr float kNoLogit = -3.0e38f;     // where the running maximum starts: a logit of -inf, masked or not, weighs nothing
@@ -260,50 +264,114 @@ __device__ __forceinline__ void put_out(const Attend& c, int64_t row, int d4, f3
 }
 __device__ __forceinline__ float natural(float m, float l) { return l > 0.f ? (m + __log2f(l)) * 0.69314718055994530942f : l == 0.f ? -INFINITY : NAN; }
 
-// One workgroup of four wavefronts per (sequence, KV head) and `piece` entries; wavefronts take blocks of 32 entries in turn.  With the rows as
+// The piece that a workgroup takes.  Where lengths decide how the work is cut they are only known here, so every workgroup looks for its own; a lane adds up its
+// share of the sequences.  Large pieces come first: the chip's last ones to end are then small.
+struct Piece {
+  int b, h, length, index, first, last, parts, part;      // blocks first .. last - 1 of the unit; piece `index` of all, `part` of the unit's `parts`
+};
+__device__ __forceinline__ int lane_at(int v, int lane) { return __builtin_amdgcn_ds_bpermute(lane << 2, v); }
+__device__ __forceinline__ bool find_piece(const Paged& p, const Attend& c, int index, int lane, int& bad, Piece& r) {
+  const int fixed = c.picked ? unit_blocks(c.n_picked << p.shift) : 0;
+  int n;
+  if (c.share) {
+    const int u = index / c.places;
+    r.part = index - u * c.places;
+    r.b = u / p.hkv;
+    r.h = u - r.b * p.hkv;
+    r.length = uniform_i32(p.length(r.b, bad));
+    n = fixed ? fixed : unit_blocks(r.length);
+    r.parts = unit_parts(n, c.share);
+    if (r.part >= r.parts) return false;
+  } else {
+    const int per_lane = (p.batch + 63) >> 6, b0 = lane * per_lane;
+    int length = 0, blocks = 0, pieces = 0, who = lane;
+    for (int i = 0; i < per_lane && b0 + i < p.batch; ++i) {
+      const int m = p.length(b0 + i, bad);
+      if (i == 0) length = m;
+      blocks += unit_blocks(m);
+    }
+    const int share = attend_share(wave_sum_i32(blocks) * p.hkv, c.workers);
+    if (per_lane == 1) {
+      pieces = unit_parts(blocks, share);
+      const int size = pieces ? unit_parts(blocks, pieces) : 0;
+      int rank = 0;
+      for (int i = 0; i < p.batch; ++i) {
+        const int other = __builtin_amdgcn_readlane(size, i);
+        rank += other > size || (other == size && i < lane);
+      }
+      who = __builtin_amdgcn_ds_permute((lane < p.batch ? rank : lane) << 2, lane);
+      pieces = lane_at(pieces, who);
+      length = lane_at(length, who);
+    } else {
+      for (int i = 0; i < per_lane && b0 + i < p.batch; ++i) pieces += unit_parts(unit_blocks(p.length(b0 + i, bad)), share);
+    }
+    pieces *= p.hkv;
+    const int upto = wave_scan_i32(pieces, lane);
+    const u64 beyond = __ballot(upto > index);
+    if (beyond == 0) return false;
+    const int ln = __ffsll((long long)beyond) - 1;
+    int before = __builtin_amdgcn_readlane(upto - pieces, ln);
+    r.b = __builtin_amdgcn_readlane(who, ln) * per_lane;
+    r.length = __builtin_amdgcn_readlane(length, ln);
+    for (;;) {
+      n = unit_blocks(r.length);
+      r.parts = unit_parts(n, share);
+      if (index < before + r.parts * p.hkv) break;
+      before += r.parts * p.hkv;
+      r.length = uniform_i32(p.length(++r.b, bad));
+    }
+    r.h = (index - before) / r.parts;
+    r.part = index - before - r.h * r.parts;
+  }
+  r.index = index;
+  const int even = n / r.parts, more = n - even * r.parts;      // the first `more` parts have a block more
+  r.first = r.part * even + min(r.part, more);
+  r.last = r.first + even + (r.part < more);
+  return true;
+}
+
+// One workgroup of four wavefronts per piece; wavefronts take blocks of 32 entries in turn.  With the rows as
 // they lie a lane (j = lane % 16, kg = lane / 16) reads of a block, per tile of 16 entries,
-//   keys    entry j, 16 bytes at 16 kg of each 64: operands of K Q^T (rows = entries) whose order of dimensions the queries share;
+//   keys    of entries 4 (j / 4) + (j / 2) % 2 and that + 2, 16 bytes at 16 (2 kg + j % 2) of each 128: every load takes whole lines (with 16 bytes of all sixteen
+//           rows it took halves: 64 sequences of 9350 entries 198 us, 269 where a slot's heads lie side by side). As operands of K Q^T (rows = entries) even rows hold
+//           other dimensions than odd ones, so that each goes with both halves of the queries and half of the results are used;
 //   values  entries 4 kg .. 4 kg + 3, the eighth of the row at j: byte (or word) moves between pairs of entries make them operands of P V (columns =
 //           dimensions 8 j + dt), in the entry order in which K Q^T leaves the logits.
 // The weights are split into bf16 terms: high ones in rows 0 .. 7 and low ones in rows 8 .. 15 of one operand for up to eight heads (the queries are
 // there twice), as operands of their own for more (WIDE).  Two terms hold 16 bits of a weight; a float output gets a third.
 template <bool E4M3, int TERMS, bool WIDE>
 __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend c) {
-  constexpr int kHeads = WIDE ? 16 : 8, kWaves = kThreads / 64, kRow = kDim + 4;
+  constexpr int kHeads = WIDE ? 16 : 8, kWaves = kAttendWaves, kRow = kDim + 4, kParts = E4M3 ? 1 : 2;
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
   __shared__ __align__(16) float s_acc[kWaves][kHeads * kRow];
-  const int u = blockIdx.x, part = blockIdx.y, b = u / p.hkv, h = u - b * p.hkv;
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i32(tid >> 6), j = lane & 15, kg = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i32(tid >> 6), j = lane & 15, kg = lane >> 4, shift = p.shift;
   int bad = 0;
-  const int length = p.length(b, bad), shift = p.shift;
-  const int total = c.picked ? c.n_picked << shift : length, e0 = part * c.piece;
-  if (e0 >= total && part > 0) return;
-  const int blocks = (min(total - e0, c.piece) + 31) >> 5;
+  Piece pc;
+  if (!find_piece(p, c, blockIdx.x, lane, bad, pc)) return;
+  const int b = pc.b, h = pc.h, u = b * p.hkv + h;
 
-  // ---- where the piece's pages lie and how far they are filled, a lane each
-  const int slot0 = e0 >> shift;
-  int page = 0, fill = 0;
-  {
-    int logical = slot0 + lane;
+  // ---- where the unit's pages lie and how far they are filled, kPageSlots of them at a time, a lane each
+  int page, fill, window = pc.first >> (shift + 1);
+  auto look_up = [&]() {
+    int logical = window * kPageSlots + lane;
     if (c.picked) logical = logical < c.n_picked ? c.picked[(int64_t)u * c.n_picked + logical] : -1;
-    if (logical < -1 || (logical >= 0 && (logical >= p.columns || page_fill(length, logical, shift) == 0))) {
-      if (c.picked) bad |= PAGED_BAD_PICK;
-      logical = -1;
+    page = logical >= 0 && logical < p.columns ? p.table[(int64_t)b * p.table_stride + logical] : 0;      // before the length is there
+    fill = logical < 0 || logical >= p.columns ? 0 : page_fill(pc.length, logical, shift);
+    if (c.picked && (logical < -1 || (logical >= 0 && fill == 0))) bad |= PAGED_BAD_PICK;
+    if (fill > 0 && !page_there(page, p.n_pages)) {
+      bad |= PAGED_BAD_PAGE;
+      fill = 0;
     }
-    if (logical >= 0) {
-      fill = page_fill(length, logical, shift);
-      page = p.page(b, logical, bad);
-      if (page < 0) page = fill = 0;
-    }
-    if (__any(bad)) p.report(bad);
-  }
+    if (fill == 0) page = 0;
+  };
+  look_up();
 
   bf16x8 q[4];
   {
     const int head = WIDE ? j : j & 7;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      const int d = E4M3 ? 64 * (s >> 1) + 16 * kg + 8 * (s & 1) : 32 * s + 8 * kg;
+      const int d = E4M3 ? 32 * kg + 16 * (s >> 1) + 8 * (s & 1) : 64 * (s & 1) + 16 * kg + 8 * (s >> 1);
       u32x4 x = {0u, 0u, 0u, 0u};
       if (head < c.G) x = load16(c.q + b * c.q_seq_stride + (h * c.G + head) * c.q_head_stride + 2 * d);
       q[s] = __builtin_bit_cast(bf16x8, x);
@@ -314,20 +382,27 @@ __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend 
   for (int dt = 0; dt < 8; ++dt) acc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m_run = kNoLogit, l_run = 0.f;
 
-  for (int blk = wave; blk < blocks; blk += kWaves) {
+  for (int blk = pc.first + wave; blk < pc.last; blk += kWaves) {
+    if (blk >> (shift + 1) != window) {
+      window = blk >> (shift + 1);
+      look_up();
+    }
     int valid[2];
     float sv[8], vs[8];
-    u32x4 kf[2][E4M3 ? 2 : 4], vf[2][4];
+    u32x4 kf[2][2][kParts], vf[2][4];
     u32x2 sc[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const int e = e0 + 32 * blk + 16 * t, off = e & ((1 << shift) - 1), at = (e >> shift) - slot0;
+      const int e = (blk << 5) + 16 * t, off = e & ((1 << shift) - 1), at = (e >> shift) & (kPageSlots - 1);
       valid[t] = min(max(__builtin_amdgcn_readlane(fill, at) - off, 0), 16);
       const int64_t pg = __builtin_amdgcn_readlane(page, at);
       const int64_t base = pg * p.page_stride + h * p.head_stride + (int64_t)off * p.slot_stride;
-      const uint8_t* kb = p.k + base + j * p.slot_stride + 16 * kg;
 #pragma unroll
-      for (int s = 0; s < (E4M3 ? 2 : 4); ++s) kf[t][s] = stream16(kb + 64 * s);
+      for (int n = 0; n < 2; ++n) {
+        const uint8_t* kb = p.k + base + (4 * (j >> 2) + ((j >> 1) & 1) + 2 * n) * p.slot_stride + 16 * (2 * kg + (j & 1));
+#pragma unroll
+        for (int s = 0; s < kParts; ++s) kf[t][n][s] = stream16(kb + 128 * s);
+      }
       const uint8_t* vb = p.v + base + 4 * kg * p.slot_stride;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -343,17 +418,24 @@ __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend 
     // ---- logits of four entries of each tile
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      f32x4 s = {0.f, 0.f, 0.f, 0.f};
+      float dot[4];
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        u32x4 x;
-        if constexpr (E4M3) {
-          const uint32_t lo = kf[t][n >> 1][2 * (n & 1)], hi = kf[t][n >> 1][2 * (n & 1) + 1];
-          x = u32x4{codes_bf16<false>(lo, 1.f), codes_bf16<true>(lo, 1.f), codes_bf16<false>(hi, 1.f), codes_bf16<true>(hi, 1.f)};
-        } else {
-          x = kf[t][n];
+      for (int n = 0; n < 2; ++n) {
+        f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          u32x4 x;
+          if constexpr (E4M3) {
+            const uint32_t lo = kf[t][n][0][2 * s], hi = kf[t][n][0][2 * s + 1];
+            x = u32x4{codes_bf16<false>(lo, 1.f), codes_bf16<true>(lo, 1.f), codes_bf16<false>(hi, 1.f), codes_bf16<true>(hi, 1.f)};
+          } else {
+            x = kf[t][n][s];
+          }
+          s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), q[s], s0, 0, 0, 0);
+          s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), q[2 + s], s1, 0, 0, 0);
         }
-        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), q[n], s, 0, 0, 0);
+        dot[2 * n] = s0[0] + s1[1];
+        dot[2 * n + 1] = s0[2] + s1[3];
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -364,7 +446,7 @@ __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend 
           k_scale *= __uint_as_float(i & 1 ? (x & 0xFF0000u) << 7 : (x & 0xFFu) << 23);
           vs[4 * t + i] = __uint_as_float(i & 1 ? (x & 0xFF000000u) >> 1 : (x & 0xFF00u) << 15);
         }
-        sv[4 * t + i] = s[i] * k_scale;
+        sv[4 * t + i] = dot[i] * k_scale;
       }
     }
     // ---- entries that are not there: logits of -inf, values and their scales of nothing (the rows may hold anything)
@@ -473,8 +555,8 @@ __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend 
       L += s_l[w][head] * f;
       y += *reinterpret_cast<const f32x4*>(&s_acc[w][head * kRow + d4]) * f;
     }
-    if (c.pieces > 1) {
-      const int64_t at = ((int64_t)u * c.pieces + part) * c.G + head;
+    if (pc.parts > 1) {
+      const int64_t at = (int64_t)pc.index * c.G + head;
       *reinterpret_cast<f32x4*>(c.partial + at * kDim + d4) = y;
       if (d4 == 0) {
         c.ml[2 * at] = M;
@@ -486,43 +568,68 @@ __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend 
       if (d4 == 0 && c.lse) c.lse[row] = natural(M, L);
     }
   }
+  if (c.parts && pc.part == 0 && tid == 0) {
+    c.parts[2 * u] = pc.index;
+    c.parts[2 * u + 1] = pc.parts;
+  }
+  p.report(bad);
 }
 
-// Joins the pieces of one (sequence, query head): eight rows of 32 threads take pieces in turn, a thread four dimensions.
-__global__ __launch_bounds__(kThreads) void paged_join_kernel(Paged p, Attend c) {
-  __shared__ float s_m[8], s_l[8];
-  __shared__ __align__(16) float s_y[8][kDim];
-  const int u = blockIdx.x, head = blockIdx.y, b = u / p.hkv, group = threadIdx.x >> 5, d4 = 4 * (threadIdx.x & 31);
-  int bad = 0;
-  const int length = p.length(b, bad), total = c.picked ? c.n_picked << p.shift : length;
-  const int pieces = min(c.pieces, (total + c.piece - 1) / c.piece);
-  float m = kNoLogit, l = 0.f;
+// Joins the pieces of units that have several: a workgroup takes `heads` query heads of a unit, eight / heads rows of 32 threads (four dimensions each) a head, a row eight
+// parts at a time.
+constexpr int kJoinRows = 8;
+__global__ __launch_bounds__(32 * kJoinRows) void paged_join_kernel(Attend c, int heads) {
+  __shared__ float s_m[kJoinRows], s_l[kJoinRows];
+  __shared__ __align__(16) float s_y[kJoinRows][kDim];
+  const int u = blockIdx.x, sides = kJoinRows / heads, row = threadIdx.x >> 5, side = row / heads, lane = threadIdx.x & 31, d4 = 4 * lane;
+  const int first = c.parts[2 * u], parts = c.parts[2 * u + 1], head = min((int)blockIdx.y * heads + row - side * heads, c.G - 1);
+  if (parts == 1) return;
+  float M = kNoLogit, L = 0.f;
   f32x4 y = {0.f, 0.f, 0.f, 0.f};
-  for (int i = group; i < pieces; i += 8) {
-    const int64_t at = ((int64_t)u * c.pieces + i) * c.G + head;
-    const f32x4 x = *reinterpret_cast<const f32x4*>(c.partial + at * kDim + d4);
-    const float mi = c.ml[2 * at], li = c.ml[2 * at + 1], M = fmaxf(m, mi), f = fast_exp2(m - M), g = fast_exp2(mi - M);
-    y = y * f + x * g;
-    l = l * f + li * g;
-    m = M;
+  auto take = [&](auto n, int i0) {                         // parts i0, i0 + sides, ..., n of them
+    constexpr int N = decltype(n)::value;
+    f32x4 x[N];
+    f32x2 st[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int64_t at = (int64_t)(first + min(i0 + k * sides, parts - 1)) * c.G + head;
+      st[k] = *reinterpret_cast<const f32x2*>(c.ml + 2 * at);
+      x[k] = *reinterpret_cast<const f32x4*>(c.partial + at * kDim + d4);
+    }
+    float m = M;
+#pragma unroll
+    for (int k = 0; k < N; ++k) m = fmaxf(m, st[k][0]);
+    const float shrink = fast_exp2(M - m);
+    M = m;
+    L *= shrink;
+    y = y * shrink;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float f = i0 + k * sides < parts ? fast_exp2(st[k][0] - m) : 0.f;
+      L += st[k][1] * f;
+      y += x[k] * f;
+    }
+  };
+  if (side < sides) {
+    int i = side;
+    for (; i - side + 2 * sides < parts; i += 8 * sides) take(std::integral_constant<int, 8>(), i);
+    if (i - side < parts) take(std::integral_constant<int, 2>(), i);
   }
-  *reinterpret_cast<f32x4*>(&s_y[group][d4]) = y;
-  if (d4 == 0) s_m[group] = m, s_l[group] = l;
+  if (lane == 0) s_m[row] = M, s_l[row] = L;
+  *reinterpret_cast<f32x4*>(&s_y[row][d4]) = y;
   __syncthreads();
-  if (group) return;
-  float M = s_m[0], L = 0.f;
-#pragma unroll
-  for (int w = 1; w < 8; ++w) M = fmaxf(M, s_m[w]);
+  if (row >= heads || (int)blockIdx.y * heads + row >= c.G) return;
+  for (int s = 1; s < sides; ++s) M = fmaxf(M, s_m[s * heads + row]);
+  L = 0.f;
   y = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int w = 0; w < 8; ++w) {
-    const float f = fast_exp2(s_m[w] - M);
-    L += s_l[w] * f;
-    y += *reinterpret_cast<const f32x4*>(&s_y[w][d4]) * f;
+  for (int s = 0; s < sides; ++s) {
+    const float f = fast_exp2(s_m[s * heads + row] - M);
+    L += s_l[s * heads + row] * f;
+    y += *reinterpret_cast<const f32x4*>(&s_y[s * heads + row][d4]) * f;
   }
-  const int64_t row = (int64_t)u * c.G + head;
-  put_out(c, row, d4, L != 0.f ? y * (1.f / L) : f32x4{0.f, 0.f, 0.f, 0.f});
-  if (d4 == 0 && c.lse) c.lse[row] = natural(M, L);
+  const int64_t to = (int64_t)u * c.G + head;
+  put_out(c, to, d4, L != 0.f ? y * (1.f / L) : f32x4{0.f, 0.f, 0.f, 0.f});
+  if (d4 == 0 && c.lse) c.lse[to] = natural(M, L);
 }
 
 // ------------------------------------------------------------------ pages picked for a token

@@ -101,14 +101,33 @@ def test_rows_of_a_call_lie_within_the_sequence_and_the_caller_s_rows(tmp_path):
                 }""")
 
 
-def test_pieces_of_an_attention_cover_it_and_know_their_pages(tmp_path):
+def test_pieces_of_an_attention_have_their_places(tmp_path):
+    """Whatever the lengths turn out to be, there are as many workgroups as pieces, and parts of the workspace for each."""
     _run(tmp_path, r"""
-  for (int shift = 4; shift <= 8; ++shift)
-    for (long long units = 1; units < 5000; units = units * 3 / 2 + 1)
-      for (long long n = 1; n <= (1 << 30); n = n * 3 / 2 + 1) {
-        const int piece = ckv::attend_piece(units, n, shift, 256), pieces = ckv::attend_pieces(n, piece);
-        if (piece < 128 || (piece & (piece - 1)) || piece > ckv::kPageSlots << shift) return std::printf("piece of %d\n", piece), 1;
-        if ((long long)pieces * piece < n || (pieces > 1 && (long long)(pieces - 1) * piece >= n)) return std::printf("%d pieces of %d for %lld\n", pieces, piece, n), 1;
+  unsigned seed = 1;
+  auto random = [&](int n) { seed = seed * 1664525u + 1013904223u; return (int)((seed >> 8) % (unsigned)n); };
+  for (long long units = 1; units < 5000; units = units * 3 / 2 + 1)
+    for (long long most = 0; most <= (1 << 30) && units * ckv::unit_blocks((int)most) <= (1 << 30); most = most * 3 / 2 + 1)
+      for (bool same : {false, true}) {
+        const ckv::AttendPlan p = ckv::attend_plan(units, (int)most, same, 256);
+        if (p.pieces < units || p.pieces > 2 * 1024 + 2 * units) return std::printf("%lld pieces of %lld units\n", p.pieces, units), 1;
+        for (int kind = 0; kind < 4; ++kind) {
+          long long pieces = 0, blocks = 0;
+          const int n = units < 100 ? (int)units : 100;          // units of so many lengths, each as often as the others
+          int length[100];
+          for (int i = 0; i < n; ++i) {
+            length[i] = kind == 0 || same ? (int)most : kind == 1 ? 0 : kind == 2 ? random((int)most + 1) : i ? random((int)most / 50 + 1) : (int)most;
+            blocks += ckv::unit_blocks(length[i]);
+          }
+          if (n < units) continue;
+          const int share = p.share ? p.share : ckv::attend_share((int)blocks, p.workers);
+          for (int i = 0; i < n; ++i) {
+            const int parts = ckv::unit_parts(ckv::unit_blocks(length[i]), share);
+            if (parts < 1 || (parts > 1 && !p.split) || (p.share && parts > p.places)) return std::printf("%d parts\n", parts), 1;
+            pieces += p.share ? p.places : parts;
+          }
+          if (pieces > p.pieces) return std::printf("%lld pieces, %lld places, %lld units of up to %lld\n", pieces, p.pieces, units, most), 1;
+        }
       }""")
 
 
