@@ -65,4 +65,16 @@ CKV_PLAN AttendPlan attend_plan(long long units, int entries, bool same, int n_c
   return {0, 0, workers, workers + units, true};
 }
 
+// Whether a selection is one kernel, a workgroup per unit, or two: scores by workgroups of so many pages, then the picking.
+constexpr int kFewPages = 512;
+CKV_PLAN bool selects_whole(int units, int columns, int n_cu) { return columns <= (units >= n_cu ? kFewPages : kFewPages / 2); }
+// Whether a selection reads bounds past the caches: not where those of several layers stay in the last one (256 MiB).  us, through / past: 64 sequences of 8 heads, 256
+// pages each (67 MB) 16.4 / 17.7, 512 (134 MB) 32.8 / 28.6, 1000 (262 MB) 63 / 54.
+CKV_PLAN bool bounds_past_caches(long long units, int columns) { return units * columns * 4 * kDim >= (96ll << 20); }
+CKV_PLAN int score_pages_each(int units, int columns, int n_cu) {
+  int each = 64;
+  while (each < 512 && (long long)units * ((columns + each - 1) / each) > 4ll * n_cu) each *= 2;
+  return each;
+}
+
 }  // namespace ckv

@@ -274,14 +274,23 @@ int ckv_paged_select(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_que
   c.keep_last = keep_last;
   c.score_stride = columns;
   const unsigned units = (unsigned)(seqs->batch * pages->n_kv_heads);
+  const int n_cu = compute_units();
+  const bool past = bounds_past_caches(units, columns);
+  if (selects_whole((int)units, columns, n_cu)) {
+    auto select = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(units), dim3(kPickThreads), 0, (hipStream_t)stream, p, c); };
+    past ? select(paged_select_kernel<true>) : select(paged_select_kernel<false>);
+    return launched("ckv_paged_select");
+  }
   if (columns > keep) {
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < score_bytes(pages, seqs)) return fail(CKV_EWORKSPACE, "workspace too small or misaligned");
-    hipLaunchKernelGGL(paged_score_kernel, dim3(units, (unsigned)((columns + kScorePages - 1) / kScorePages)), dim3(kThreads), 0, (hipStream_t)stream, p, c);
+    const int each = score_pages_each((int)units, columns, n_cu);
+    const dim3 grid(units, (unsigned)((columns + each - 1) / each));
+    auto score = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, (hipStream_t)stream, p, c, each); };
+    past ? score(paged_score_kernel<true>) : score(paged_score_kernel<false>);
     if (int rc = launched("ckv_paged_select")) return rc;
   }
   auto pick = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(units), dim3((unsigned)threads), 0, (hipStream_t)stream, p, c); };
-  if (columns <= kThreads) pick(paged_pick_kernel<1, kThreads>, kThreads);
-  else if (columns <= 4 * kThreads) pick(paged_pick_kernel<4, kThreads>, kThreads);
+  if (columns <= 4 * kThreads) pick(paged_pick_kernel<4, kThreads>, kThreads);
   else if (columns <= 4 * kWideThreads) pick(paged_pick_kernel<4, kWideThreads>, kWideThreads);
   else if (columns <= 8 * kWideThreads) pick(paged_pick_kernel<8, kWideThreads>, kWideThreads);
   else pick(paged_pick_kernel<32, kWideThreads>, kWideThreads);

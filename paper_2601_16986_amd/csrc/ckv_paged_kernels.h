@@ -644,7 +644,32 @@ struct Select {
 // A page's score is the sum over the group's heads of the largest logit that its extremes allow, sum_d max(q_d min_d, q_d max_d): with the heads'
 // positive and negative parts summed beforehand one product of 256 terms.  In 64 bits, because scores decide: whoever adds up in another order gets the same
 // pages.  Sixteen lanes take a page, 8 dimensions of both extremes each.
-constexpr int kScorePages = 64;        // per workgroup
+struct Parts {
+  double up[8], down[8];
+};
+__device__ __forceinline__ Parts query_parts(const Paged& p, const Select& c, int b, int h, int piece) {
+  Parts r;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r.up[i] = r.down[i] = 0.0;
+  const uint8_t* q = c.q + b * c.q_seq_stride + h * c.G * c.q_head_stride + 16 * piece;
+  for (int g0 = 0; g0 < c.G; g0 += 8) {
+    u32x4 x[8];
+#pragma unroll
+    for (int g = 0; g < 8; ++g) x[g] = load16(q + min(g0 + g, c.G - 1) * c.q_head_stride);      // all on their way before the first is looked at
+#pragma unroll
+    for (int g = 0; g < 8; ++g) {
+      if (g0 + g >= c.G) break;
+      float y[8];
+      unpack8(x[g], y);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        r.up[i] += y[i] < 0.f ? 0.f : y[i];
+        r.down[i] += y[i] < 0.f ? y[i] : 0.f;
+      }
+    }
+  }
+  return r;
+}
 
 // Sum over the lane's row of 16 lanes.
 __device__ __forceinline__ double row_sum(double s) {
@@ -654,46 +679,58 @@ __device__ __forceinline__ double row_sum(double s) {
   return s + dpp_f64<kDppRowMirror>(s);
 }
 
-__global__ __launch_bounds__(kThreads) void paged_score_kernel(Paged p, Select c) {
-  const int u = blockIdx.x, b = u / p.hkv, h = u - b * p.hkv, piece = threadIdx.x & 15, group = threadIdx.x >> 4;
-  int bad = 0;
-  const int length = p.length(b, bad), held = (int)(((int64_t)length + p.page_size() - 1) >> p.shift), first = blockIdx.y * kScorePages;
-  if (first >= held || held <= c.keep) return;
-  double up[8], down[8];
+// Scores of the sequence's pages first, first + step, ... (N of them, as far as there are so many) to put(page, score).
+template <int N, bool PAST, class Put>
+__device__ __forceinline__ void score_pages(const Paged& p, int b, int h, int held, int first, int step, const Parts& q, int piece, int& bad, Put put) {
+  int page[N];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) up[i] = down[i] = 0.0;
-  for (int g = 0; g < c.G; ++g) {
-    float x[8];
-    unpack8(load16(c.q + b * c.q_seq_stride + (h * c.G + g) * c.q_head_stride + 16 * piece), x);
+  for (int n = 0; n < N; ++n) page[n] = p.table[(int64_t)b * p.table_stride + min(first + n * step, held - 1)];
+  u32x4 least[N], most[N];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      up[i] += x[i] < 0.f ? 0.f : x[i];
-      down[i] += x[i] < 0.f ? x[i] : 0.f;
+  for (int n = 0; n < N; ++n) {
+    if (!page_there(page[n], p.n_pages)) {
+      if (first + n * step < held) bad |= PAGED_BAD_PAGE;
+      page[n] = -1;
     }
+    const uint8_t* from = p.bounds + max(page[n], 0) * p.bounds_page_stride + h * p.bounds_head_stride + 16 * piece;
+    least[n] = PAST ? stream16(from) : load16(from);
+    most[n] = PAST ? stream16(from + 2 * kDim) : load16(from + 2 * kDim);
   }
 #pragma unroll
-  for (int n = 0; n < kScorePages / 16; ++n) {
-    const int at = first + 16 * n + group;
-    const int page = at < held ? p.page(b, at, bad) : -1;
-    const uint8_t* from = p.bounds + max(page, 0) * p.bounds_page_stride + h * p.bounds_head_stride + 16 * piece;
+  for (int n = 0; n < N; ++n) {
     float lo[8], hi[8];
-    unpack8(load16(from), lo);
-    unpack8(load16(from + 2 * kDim), hi);
+    unpack8(least[n], lo);
+    unpack8(most[n], hi);
     double s = 0.0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s = fma((double)hi[i], up[i], fma((double)lo[i], down[i], s));
+    for (int i = 0; i < 8; ++i) s = fma((double)hi[i], q.up[i], fma((double)lo[i], q.down[i], s));
     s = row_sum(s);
     if (__any(s != s)) {                  // infinite extremes: where no query has a part of that sign the product is nothing
       s = 0.0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        if (up[i] != 0.0) s += hi[i] * up[i];
-        if (down[i] != 0.0) s += lo[i] * down[i];
+        if (q.up[i] != 0.0) s += hi[i] * q.up[i];
+        if (q.down[i] != 0.0) s += lo[i] * q.down[i];
       }
       s = row_sum(s);
     }
-    if (piece == 0 && at < held) c.scores[(int64_t)u * c.score_stride + at] = page < 0 ? -INFINITY : (float)s;
+    if (piece == 0 && first + n * step < held) put(first + n * step, page[n] < 0 ? -INFINITY : (float)s);
   }
+}
+__device__ __forceinline__ int pages_held(const Paged& p, int length) { return (int)(((int64_t)length + p.page_size() - 1) >> p.shift); }
+
+// A workgroup takes `each` pages of a unit, 64 at a time.  PAST: extremes are read past the caches (bounds_past_caches).
+template <bool PAST>
+__global__ __launch_bounds__(kThreads) void paged_score_kernel(Paged p, Select c, int each) {
+  const int u = blockIdx.x, b = u / p.hkv, h = u - b * p.hkv, piece = threadIdx.x & 15, group = threadIdx.x >> 4;
+  int bad = 0;
+  const int held = pages_held(p, p.length(b, bad)), first = blockIdx.y * each;
+  if (first >= held || held <= c.keep) return;
+  const Parts q = query_parts(p, c, b, h, piece);
+  float* to = c.scores + (int64_t)u * c.score_stride;
+  const int last = min(first + each, held);
+  for (int at = first; at < last; at += 64)
+    score_pages<4, PAST>(p, b, h, last, at + group, 16, q, piece, bad, [&](int page, float s) { to[page] = s; });
   if (piece == 0) p.report(bad);
 }
 
@@ -704,53 +741,83 @@ __device__ __forceinline__ uint32_t score_key(float s) {
   return ~(x & 0x80000000u ? ~x : x | 0x80000000u);
 }
 
-// One workgroup per (sequence, KV head), R consecutive pages per thread: the first and last ones, and of the others those with the best scores (ties: lowest
-// page), in ascending order.
+// The first and last pages of a unit, and of the others those with the best scores (ties: lowest page), in ascending order, by a workgroup of NT threads with R
+// consecutive pages each.
+template <int NT>
+struct PickBuf {
+  CutBuf cut;
+  int count[NT / 64];
+};
 template <int R, int NT>
-__global__ __launch_bounds__(NT) void paged_pick_kernel(Paged p, Select c) {
-  __shared__ CutBuf cb;
-  __shared__ int s_count[NT / 64];
-  const int u = blockIdx.x, b = u / p.hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int bad = 0;
-  const int length = p.length(b, bad), held = (int)(((int64_t)length + p.page_size() - 1) >> p.shift);
-  if (tid == 0) p.report(bad);
+__device__ __forceinline__ void pick_pages(const Select& c, int u, int held, const float* scores, PickBuf<NT>& pb, int tid) {
+  const int lane = tid & 63, wave = tid >> 6;
   int32_t* to = c.picked + (int64_t)u * c.keep;
   if (held <= c.keep) {
     for (int i = tid; i < c.keep; i += NT) to[i] = i < held ? i : -1;
     return;
   }
+  auto open = [&](int at) { return at >= c.keep_first && at < held - c.keep_last; };
   uint32_t key[R], index[R];
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int at = tid * R + i;
-    const bool open = at >= c.keep_first && at < held - c.keep_last;
     index[i] = (uint32_t)at;
-    key[i] = open ? score_key(c.scores[(int64_t)u * c.score_stride + at]) : 0xFFFFFFFFu;
+    key[i] = open(at) ? score_key(scores[at]) : 0xFFFFFFFFu;
   }
   const int want = c.keep - c.keep_first - c.keep_last;
   KeyCut cut{0u, 0u};
-  if (want > 0) cut = select_low_keys<R, NT>(key, index, want, cb, tid);
+  if (want > 0) cut = select_low_keys<R, NT>(key, index, want, pb.cut, tid);
   int mine = 0;
   uint32_t taken = 0u;
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int at = tid * R + i;
-    const bool open = at >= c.keep_first && at < held - c.keep_last;
-    const bool take = at < held && (!open || (want > 0 && cut(key[i], index[i])));
+    const bool take = at < held && (!open(at) || (want > 0 && cut(key[i], index[i])));
     taken |= (take ? 1u : 0u) << i;
     mine += take;
   }
   const int upto = wave_scan_i32(mine, lane);
-  if (lane == 63) s_count[wave] = upto;
+  if (lane == 63) pb.count[wave] = upto;
   __syncthreads();
   int at = upto - mine;
-  for (int w = 0; w < wave; ++w) at += s_count[w];
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) at += w < wave ? pb.count[w] : 0;
 #pragma unroll
   for (int i = 0; i < R; ++i)
     if (taken >> i & 1u) {
       if (at < c.keep) to[at] = tid * R + i;
       ++at;
     }
+}
+
+template <int R, int NT>
+__global__ __launch_bounds__(NT) void paged_pick_kernel(Paged p, Select c) {
+  __shared__ PickBuf<NT> pb;
+  const int u = blockIdx.x, b = u / p.hkv, tid = threadIdx.x;
+  int bad = 0;
+  const int held = pages_held(p, p.length(b, bad));
+  if (tid == 0) p.report(bad);
+  pick_pages<R, NT>(c, u, held, c.scores + (int64_t)u * c.score_stride, pb, tid);
+}
+
+// Scores and picking by one workgroup per unit, where units have few pages.
+constexpr int kPickThreads = 512;
+template <bool PAST>
+__global__ __launch_bounds__(kPickThreads) void paged_select_kernel(Paged p, Select c) {
+  __shared__ PickBuf<kPickThreads> pb;
+  __shared__ float s_scores[kFewPages];
+  const int u = blockIdx.x, b = u / p.hkv, h = u - b * p.hkv, tid = threadIdx.x, piece = tid & 15, group = tid >> 4;
+  constexpr int kGroups = kPickThreads / 16;
+  int bad = 0;
+  const int held = pages_held(p, p.length(b, bad));
+  if (held > c.keep) {
+    const Parts q = query_parts(p, c, b, h, piece);
+    for (int first = group; first < held; first += 4 * kGroups)
+      score_pages<4, PAST>(p, b, h, held, first, kGroups, q, piece, bad, [&](int page, float s) { s_scores[page] = s; });
+    __syncthreads();
+  }
+  p.report(bad);
+  pick_pages<kFewPages / kPickThreads, kPickThreads>(c, u, held, s_scores, pb, tid);
 }
 
 }  // namespace ckv
