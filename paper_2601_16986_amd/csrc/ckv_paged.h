@@ -36,6 +36,17 @@ CKV_PLAN RowSpan row_span(int length, int most, bool has_first, int first, bool 
   return {first, count, false};
 }
 
+// Whether a page's rows are written by one wavefront instead of four, where pages are enough to fill the chip all the same and have few new rows: the smallest
+// pages, or up to four rows a sequence (one pass either way). us, four / one: prompts of 8 x 9350 over 8 heads, pages of 16 80.7 / 63.3, of 32 62.6 / 63.5, of 64
+// 60.5 / 68; 32 prompts of up to 1000, pages of 16, 26.9 / 16.3; one of 777 over 4 heads (196 pages) 4.1 / 5.0; single rows of 32 x 8 4.0 / 4.2, 256 x 8 7.3 / 5.1.
+CKV_PLAN bool appends_by_wave(int page_size, int rows, long long pages, int n_cu) {
+  return page_size == kMinPage ? pages >= 16ll * n_cu : rows <= 4 && pages >= 4ll * n_cu;
+}
+
+// Whether rows that are read back (so many keys, and as many values) are stored past the caches: where they would fill a good part of the last one (256 MiB). us,
+// through / past: 322208 rows (165 MB) 55.8 / 49.9 out of 8 bits, 71.6 / 68.2 out of bf16; 72192 rows (37 MB) 11.7 / 11.6.
+CKV_PLAN bool reads_past_caches(long long rows) { return rows * kDim * 4 >= (64ll << 20); }
+
 // An attention's work in blocks of 32 entries: one for a unit (sequence, KV head) without entries, whose output somebody has to write.
 constexpr int kAttendWaves = 4;         // of a workgroup, which take blocks in turn
 CKV_PLAN int unit_blocks(int entries) { return entries > 32 ? (int)(((long long)entries + 31) / 32) : 1; }

@@ -175,8 +175,10 @@ int ckv_paged_append(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_row
   const long long reach = std::min<long long>(rows->rows, seqs->max_length), touched = std::min<long long>((reach + pages->page_size - 2) / pages->page_size + 1, seqs->columns);
   if (touched > kMaxGrid) return fail(CKV_EINVAL, "rows of a call may reach 65535 pages of a sequence at most");
   const dim3 grid((unsigned)(seqs->batch * pages->n_kv_heads), (unsigned)touched);
-  if (pages->dtype == CKV_E4M3) hipLaunchKernelGGL(paged_append_kernel<true>, grid, dim3(kThreads), 0, (hipStream_t)stream, p, r);
-  else hipLaunchKernelGGL(paged_append_kernel<false>, grid, dim3(kThreads), 0, (hipStream_t)stream, p, r);
+  auto launch = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, grid, dim3((unsigned)threads), 0, (hipStream_t)stream, p, r); };
+  const bool e4m3 = pages->dtype == CKV_E4M3;
+  if (appends_by_wave(pages->page_size, rows->rows, (long long)grid.x * grid.y, compute_units())) e4m3 ? launch(paged_append_kernel<true, 64>, 64) : launch(paged_append_kernel<false, 64>, 64);
+  else e4m3 ? launch(paged_append_kernel<true, kThreads>, kThreads) : launch(paged_append_kernel<false, kThreads>, kThreads);
   return launched("ckv_paged_append");
 }
 
@@ -189,8 +191,10 @@ int ckv_paged_read(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_rows*
   const long long pieces = (std::min<long long>(rows->rows, seqs->max_length) + kReadRows - 1) / kReadRows;
   if (pieces > kMaxGrid) return fail(CKV_EINVAL, "too many rows for one call");
   const dim3 grid((unsigned)(seqs->batch * pages->n_kv_heads), (unsigned)pieces);
-  if (pages->dtype == CKV_E4M3) hipLaunchKernelGGL(paged_read_kernel<true>, grid, dim3(kThreads), 0, (hipStream_t)stream, p, r);
-  else hipLaunchKernelGGL(paged_read_kernel<false>, grid, dim3(kThreads), 0, (hipStream_t)stream, p, r);
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, (hipStream_t)stream, p, r); };
+  const bool past = reads_past_caches((rows->starts ? (long long)rows->total : (long long)seqs->batch * std::min(rows->rows, seqs->max_length)) * pages->n_kv_heads);
+  if (pages->dtype == CKV_E4M3) past ? launch(paged_read_kernel<true, true>) : launch(paged_read_kernel<true, false>);
+  else past ? launch(paged_read_kernel<false, true>) : launch(paged_read_kernel<false, false>);
   return launched("ckv_paged_read");
 }
 

@@ -82,37 +82,17 @@ struct Rows {
   }
 };
 
-// Largest of the lane's row of 16 lanes.
-__device__ __forceinline__ float row_max(float v) {
-  v = fmaxf(v, __int_as_float(dpp_i32<kDppQuadSwap1>(__float_as_int(v))));
-  v = fmaxf(v, __int_as_float(dpp_i32<kDppQuadSwap2>(__float_as_int(v))));
-  v = fmaxf(v, __int_as_float(dpp_i32<kDppRowHalfMirror>(__float_as_int(v))));
-  return fmaxf(v, __int_as_float(dpp_i32<kDppRowMirror>(__float_as_int(v))));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pk_max_u16(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
 }
-
-// Eight values of a row that 16 lanes hold, to codes: E = the smallest integer for which the row's largest finite magnitude is at most
-// 448 * 2^E, from -100 to 120 (so that codes times 2^E stay normal bf16 numbers).  448 = 1.75 * 2^8, so E follows from the magnitude's exponent and its first two bits of
-// mantissa.  x * 2^-E is exact, the conversion rounds to nearest, ties to even; what is no number or infinite becomes the format's NaN.
-__device__ __forceinline__ u32x2 quantise8(const float (&x)[8], int& e) {
-  float big = 0.f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float a = fabsf(x[i]);
-    big = fmaxf(big, a < INFINITY ? a : 0.f);
-  }
-  const uint32_t bits = __float_as_uint(row_max(big));
-  e = min(max((int)(bits >> 23) - 127 - 8 + ((bits & 0x7FFFFFu) > 0x600000u), -100), 120);
-  const float inverse = __uint_as_float((uint32_t)(127 - e) << 23);
-  float y[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = fabsf(x[i]) < INFINITY ? x[i] * inverse : NAN;
-  u32x2 codes;
-#pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    int c = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * w], y[4 * w + 1], 0, false);
-    codes[w] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * w + 2], y[4 * w + 3], c, true);
-  }
-  return codes;
+// Largest of the lane's row of 16 lanes.
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+  v = max(v, (uint32_t)dpp_i32<kDppQuadSwap1>((int)v));
+  v = max(v, (uint32_t)dpp_i32<kDppQuadSwap2>((int)v));
+  v = max(v, (uint32_t)dpp_i32<kDppRowHalfMirror>((int)v));
+  return max(v, (uint32_t)dpp_i32<kDppRowMirror>((int)v));
 }
 
 __device__ __forceinline__ void unpack8(u32x4 x, float (&f)[8]) {
@@ -122,15 +102,55 @@ __device__ __forceinline__ void unpack8(u32x4 x, float (&f)[8]) {
     f[2 * i + 1] = bf16_high(x[i]);
   }
 }
+
+constexpr uint32_t kInfinite = 0x7F80u;       // a bf16's magnitude from which it is not finite
+// Largest magnitude (its bits) of a row that 16 lanes hold, 8 values each; with infinities and NaN if there are any.
+__device__ __forceinline__ uint32_t magnitude(u32x4 x) {
+  constexpr uint32_t kBits = 0x7FFF7FFFu;
+  const uint32_t m = pk_max_u16(pk_max_u16(x[0] & kBits, x[1] & kBits), pk_max_u16(x[2] & kBits, x[3] & kBits));
+  return row_max(max(m & 0xFFFFu, m >> 16));
+}
+// The row without what is not finite, as NaN for the codes.
+__device__ __forceinline__ u32x4 finite8(u32x4 x, uint32_t instead) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((x[i] & 0x7F80u) == 0x7F80u) x[i] = (x[i] & 0xFFFF0000u) | instead;
+    if ((x[i] & 0x7F800000u) == 0x7F800000u) x[i] = (x[i] & 0xFFFFu) | instead << 16;
+  }
+  return x;
+}
+// Eight values of a row that 16 lanes hold, to codes and the scale's byte E + 127: E = the smallest integer for which the row's largest finite magnitude is at most
+// 448 * 2^E, from -100 to 120 (so that codes times 2^E stay normal bf16 numbers).  448 = 1.75 * 2^8, so E follows from the magnitude's bits: its exponent less 8, one more
+// if its mantissa is above 0x60.  x / 2^E is exact, the conversion rounds to nearest, ties to even; what is no number or infinite becomes the format's NaN.
+__device__ __forceinline__ u32x2 quantise8(u32x4 x, uint32_t& e) {
+  uint32_t m = magnitude(x);
+  if (__any(m >= kInfinite)) {
+    m = magnitude(finite8(x, 0u));
+    x = finite8(x, 0x7FC0u);
+  }
+  e = (uint32_t)min(max((int)((m + 0x1Fu) >> 7) - 8, 127 - 100), 127 + 120);
+  const float scale = __uint_as_float(e << 23);
+  u32x2 codes;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    const uint32_t a = x[2 * w], z = x[2 * w + 1];       // (a bit cast of a vector's element itself takes the first)
+    i16x2 c = {0, 0};
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c, __builtin_bit_cast(bf16x2, a), scale, false);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c, __builtin_bit_cast(bf16x2, z), scale, true);
+    codes[w] = __builtin_bit_cast(uint32_t, c);
+  }
+  return codes;
+}
+
 __device__ __forceinline__ u32x4 values8(u32x2 codes, float scale) {
   return u32x4{codes_bf16<false>(codes[0], scale), codes_bf16<true>(codes[0], scale), codes_bf16<false>(codes[1], scale), codes_bf16<true>(codes[1], scale)};
 }
 
 // One workgroup per (sequence, KV head) and page that new rows reach: it alone touches the page's rows and extremes, so that these need no atomics.  Sixteen
 // lanes take a row, 16 bytes of bf16 each, for key and value.
-template <bool E4M3>
-__global__ __launch_bounds__(kThreads) void paged_append_kernel(Paged p, Rows r) {
-  __shared__ float s_lo[kThreads / 64][kDim], s_hi[kThreads / 64][kDim];
+template <bool E4M3, int NT>
+__global__ __launch_bounds__(NT) void paged_append_kernel(Paged p, Rows r) {
+  __shared__ float s_lo[NT / 64][kDim], s_hi[NT / 64][kDim];
   const int u = blockIdx.x, b = u / p.hkv, h = u - b * p.hkv;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, piece = lane & 15, group = tid >> 4;
   int bad = 0;
@@ -151,32 +171,30 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(Paged p, Rows r)
   float lo[8], hi[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) lo[i] = INFINITY, hi[i] = -INFINITY;
-  for (int row = begin + group; row < end; row += kThreads / 16) {
+  for (int row = begin + group; row < end; row += NT / 16) {
     const int64_t from = base + (int64_t)(row - span.first) * r.row_stride + h * r.head_stride + 16 * piece;
     const int slot = row & (p.page_size() - 1);
     u32x4 k = load16(r.k + from), v = load16(r.v + from);
     if constexpr (E4M3) {
-      float x[8];
-      int ek, ev;
-      unpack8(k, x);
-      const u32x2 ck = quantise8(x, ek);
-      unpack8(v, x);
-      const u32x2 cv = quantise8(x, ev);
+      uint32_t ek, ev;
+      const u32x2 ck = quantise8(k, ek), cv = quantise8(v, ev);
       const int64_t to = at + (int64_t)slot * p.slot_stride + 8 * piece;
       *reinterpret_cast<u32x2*>(p.k + to) = ck;
       *reinterpret_cast<u32x2*>(p.v + to) = cv;
       if (piece == 0)
-        *reinterpret_cast<uint16_t*>(p.scales + page * p.scale_page_stride + h * p.scale_head_stride + 2 * slot) = (uint16_t)((ek + 127) | (ev + 127) << 8);
-      k = values8(ck, __uint_as_float((uint32_t)(ek + 127) << 23));
+        *reinterpret_cast<uint16_t*>(p.scales + page * p.scale_page_stride + h * p.scale_head_stride + 2 * slot) = (uint16_t)(ek | ev << 8);
+      k = values8(ck, __uint_as_float(ek << 23));
     } else {
       const int64_t to = at + (int64_t)slot * p.slot_stride + 16 * piece;
       *reinterpret_cast<u32x4*>(p.k + to) = k;
       *reinterpret_cast<u32x4*>(p.v + to) = v;
     }
-    float x[8];
-    unpack8(k, x);
+    if (p.bounds) {
+      float x[8];
+      unpack8(k, x);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) lo[i] = fminf(lo[i], x[i]), hi[i] = fmaxf(hi[i], x[i]);
+      for (int i = 0; i < 8; ++i) lo[i] = fminf(lo[i], x[i]), hi[i] = fmaxf(hi[i], x[i]);
+    }
   }
   if (!p.bounds) return;
 #pragma unroll
@@ -189,47 +207,72 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(Paged p, Rows r)
     for (int i = 0; i < 8; ++i) s_lo[wave][8 * piece + i] = lo[i], s_hi[wave][8 * piece + i] = hi[i];
   }
   __syncthreads();
-  if (tid >= 2 * kDim) return;
-  const int d = tid & (kDim - 1), side = tid >> 7;       // threads 0 .. 127 the least values, 128 .. 255 the largest
-  const float(*s)[kDim] = side ? s_hi : s_lo;
-  uint16_t* to = reinterpret_cast<uint16_t*>(p.bounds + page * p.bounds_page_stride + h * p.bounds_head_stride) + tid;
-  float x = s[0][d];
 #pragma unroll
-  for (int w = 1; w < kThreads / 64; ++w) x = side ? fmaxf(x, s[w][d]) : fminf(x, s[w][d]);
-  if (begin & (p.page_size() - 1)) {                       // rows that were there before
-    const float old = __uint_as_float((uint32_t)*to << 16);
-    x = side ? fmaxf(x, old) : fminf(x, old);
+  for (int i = tid; i < 2 * kDim; i += NT) {             // 0 .. 127 the least values, 128 .. 255 the largest
+    const int d = i & (kDim - 1), side = i >> 7;
+    const float(*s)[kDim] = side ? s_hi : s_lo;
+    uint16_t* to = reinterpret_cast<uint16_t*>(p.bounds + page * p.bounds_page_stride + h * p.bounds_head_stride) + i;
+    float x = s[0][d];
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) x = side ? fmaxf(x, s[w][d]) : fminf(x, s[w][d]);
+    if (begin & (p.page_size() - 1)) {                     // rows that were there before
+      const float old = __uint_as_float((uint32_t)*to << 16);
+      x = side ? fmaxf(x, old) : fminf(x, old);
+    }
+    *to = (uint16_t)(__float_as_uint(x) >> 16);            // a bf16 value as it is
   }
-  *to = (uint16_t)(__float_as_uint(x) >> 16);              // a bf16 value as it is
 }
 
-// Sixteen lanes take a row, 64 rows per workgroup.
-constexpr int kReadRows = 64;
-template <bool E4M3>
+// Sixteen lanes take a row, 32 rows per workgroup, two of them asked for at once.  PAST: rows are stored past the caches (reads_past_caches).
+constexpr int kReadRows = 32;
+template <bool E4M3, bool PAST>
 __global__ __launch_bounds__(kThreads) void paged_read_kernel(Paged p, Rows r) {
   const int u = blockIdx.x, b = u / p.hkv, h = u - b * p.hkv, piece = threadIdx.x & 15, group = threadIdx.x >> 4;
   int bad = 0;
-  const int length = p.length(b, bad);
+  const int length = uniform_i32(p.length(b, bad));
   int64_t base;
-  const RowSpan span = r.span(b, length, base);
-  if (span.bad) bad |= PAGED_BAD_LENGTH;
+  const RowSpan rows = r.span(b, length, base);
+  if (rows.bad) bad |= PAGED_BAD_LENGTH;
+  const int first = blockIdx.y * kReadRows;
+  if (first >= rows.count) {
+    if (blockIdx.y == 0 && threadIdx.x == 0) p.report(bad);
+    return;
+  }
+  constexpr int N = kReadRows / 16;
+  int page[N];
+  u32x4 k[N], v[N];
+  uint32_t s[N];
 #pragma unroll
-  for (int n = 0; n < kReadRows / 16; ++n) {
-    const int i = blockIdx.y * kReadRows + 16 * n + group;
-    if (i >= span.count) break;
-    const int row = span.first + i, slot = row & (p.page_size() - 1);
-    const int page = p.page(b, row >> p.shift, bad);
-    if (page < 0) continue;
-    const int64_t from = page * p.page_stride + h * p.head_stride + (int64_t)slot * p.slot_stride;
+  for (int n = 0; n < N; ++n) page[n] = p.page(b, (rows.first + min(first + 16 * n + group, rows.count - 1)) >> p.shift, bad);
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int slot = (rows.first + min(first + 16 * n + group, rows.count - 1)) & (p.page_size() - 1);
+    const int64_t pg = max(page[n], 0), from = pg * p.page_stride + h * p.head_stride + (int64_t)slot * p.slot_stride;
+    if constexpr (E4M3) {
+      const u32x2 a = load8(p.k + from + 8 * piece), z = load8(p.v + from + 8 * piece);
+      k[n] = u32x4{a[0], a[1], 0u, 0u};
+      v[n] = u32x4{z[0], z[1], 0u, 0u};
+      s[n] = *reinterpret_cast<const uint16_t*>(p.scales + pg * p.scale_page_stride + h * p.scale_head_stride + 2 * slot);
+    } else {
+      k[n] = load16(p.k + from + 16 * piece);
+      v[n] = load16(p.v + from + 16 * piece);
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int i = first + 16 * n + group;
+    if (i >= rows.count || page[n] < 0) continue;
     const int64_t to = base + (int64_t)i * r.row_stride + h * r.head_stride + 16 * piece;
     if constexpr (E4M3) {
-      const uint32_t s = *reinterpret_cast<const uint16_t*>(p.scales + page * p.scale_page_stride + h * p.scale_head_stride + 2 * slot);
-      const u32x2 k = load8(p.k + from + 8 * piece), v = load8(p.v + from + 8 * piece);
-      *reinterpret_cast<u32x4*>(r.k + to) = values8(k, __uint_as_float((s & 0xFF) << 23));
-      *reinterpret_cast<u32x4*>(r.v + to) = values8(v, __uint_as_float((s >> 8) << 23));
+      k[n] = values8(u32x2{k[n][0], k[n][1]}, __uint_as_float((s[n] & 0xFF) << 23));
+      v[n] = values8(u32x2{v[n][0], v[n][1]}, __uint_as_float((s[n] >> 8) << 23));
+    }
+    if constexpr (PAST) {
+      __builtin_nontemporal_store(k[n], reinterpret_cast<u32x4*>(r.k + to));
+      __builtin_nontemporal_store(v[n], reinterpret_cast<u32x4*>(r.v + to));
     } else {
-      *reinterpret_cast<u32x4*>(r.k + to) = load16(p.k + from + 16 * piece);
-      *reinterpret_cast<u32x4*>(r.v + to) = load16(p.v + from + 16 * piece);
+      *reinterpret_cast<u32x4*>(r.k + to) = k[n];
+      *reinterpret_cast<u32x4*>(r.v + to) = v[n];
     }
   }
   if (piece == 0) p.report(bad);

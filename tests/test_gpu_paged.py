@@ -520,3 +520,18 @@ def test_a_paged_prompt_beside_and_into_a_budgeted_cache():
     g8.load_prompt(0, *(x.transpose(1, 2).contiguous() for x in e.cache.read(e.seqs, n)))
     g8.evict()
     assert g8.status() == 0 and (g8.lengths() == 256).all()
+
+
+def test_rows_of_many_sequences_and_of_many_small_pages():
+    """Enough pages that a wavefront takes one each: single rows of 600 sequences, and a long prompt in pages of 16."""
+    for lengths, ps, rows in (([1 + i % 60 for i in range(600)], 32, 1), ([9000, 8000], 16, 9000)):
+        f = Filled(lengths, 4, ps, True, seed=rows)
+        _check_pools(f)
+        if rows == 1:
+            g = Filled(lengths, 4, ps, True, seed=rows)
+            k, v = (torch.from_numpy(np.stack([x[b, n - 1] for b, n in enumerate(lengths)])).to(DEV).bfloat16() for x in f.rows)
+            for x in (g.cache.k, g.cache.v):
+                for b, n in enumerate(lengths):
+                    x.view(torch.uint8)[g.table[b, (n - 1) // ps], :, (n - 1) % ps] = 0
+            g.cache.append(g.seqs, k, v)
+            _check_pools(g)
