@@ -442,15 +442,15 @@ int ckv_paged_append(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_row
 /* Reads rows back as bf16 (exact: see ckv_pages). */
 int ckv_paged_read(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_rows* rows, void* stream);
 
-/* Bytes of workspace that ckv_paged_attend (n_picked pages per KV head, 0: all entries) and ckv_paged_select need for these sizes on the
- * current device; it depends on max_length and the sizes alone.  0 if they are refused. */
+/* Bytes of workspace that ckv_paged_attend needs (n_picked pages per KV head, 0: all entries), or ckv_paged_select (n_picked = -1), for these
+ * sizes on the current device; it depends on max_length and the sizes alone.  256 if none is needed, 0 if the sizes are refused. */
 size_t ckv_paged_workspace_bytes(const ckv_pages* pages, const ckv_seqs* seqs, int32_t n_q_heads, int32_t n_picked);
 
 /* Attention of one new token per sequence (whose own row has been appended): out[b][g] = softmax(softmax_scale q K^T) V over the sequence's
  * entries, out dev out_dtype [batch][n_q_heads][128]; lse (dev float [batch][n_q_heads], or NULL) the natural logarithm of the sum of the
  * exponentials, with which partial attentions can be joined.  A sequence without entries gets zeros and -inf; so does a head all of whose
  * logits are -inf.  With `picked` (dev [batch][n_kv_heads][n_picked], as ckv_paged_select leaves it) only the entries of the listed pages of the
- * sequence take part; -1 stands for no page, the order does not matter, and a page listed twice counts twice.  workspace: 256-byte aligned, not needed where
+ * sequence take part; -1 stands for no page, the order does not matter, and a page listed twice counts twice.  workspace: 256-byte aligned, NULL where
  * ckv_paged_workspace_bytes says 256.  Values of entries in use must be finite. */
 int ckv_paged_attend(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_query* query, float softmax_scale, const int32_t* picked,
                      int32_t n_picked, void* out, int32_t out_dtype, float* lse, void* workspace, size_t workspace_bytes, void* stream);

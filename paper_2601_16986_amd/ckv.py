@@ -522,6 +522,7 @@ class PagedCache:
         if self.device.type != "cuda":
             raise CkvError(EINVAL, f"the pools must be device memory, not on {self.device}")
         self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._like = torch.empty(0, dtype=torch.bfloat16, device=self.device)
         self._index = self.device.index if self.device.index is not None else 0
         self._struct = Pages(self.n_pages, self.page_size, self.n_kv_heads, self.head_dim, self.dtype, _stride(k, 0, self.head_dim), _stride(k, 1, self.head_dim),
                              k.stride(2), *s, *b, k.data_ptr(), v.data_ptr(), scales.data_ptr() if scales is not None else None,
@@ -548,16 +549,18 @@ class PagedCache:
 
     def _call(self, entry, *args):
         """entry(*args, stream) on the pools' device."""
-        cuda = self.torch.cuda
-        if self._raw_stream is not None and cuda.current_device() == self._index:
-            rc = entry(*args, self._raw_stream(self._index))
+        index = self._index
+        if self._raw_stream is not None and self.torch.cuda.current_device() == index:
+            rc = entry(*args, self._raw_stream(index))
         else:
-            with cuda.device(self.device):
-                rc = entry(*args, cuda.current_stream(self.device).cuda_stream)
+            with self.torch.cuda.device(self.device):
+                rc = entry(*args, self.torch.cuda.current_stream(self.device).cuda_stream)
         if rc != OK:
             raise CkvError(rc, self.lib.ckv_last_error(None).decode())
 
-    def _workspace(self, seqs, n_q_heads, n_picked, least=256):
+    def _workspace(self, seqs, n_q_heads, n_picked):
+        """(tensor, address, bytes) of a workspace for a call of these sizes, from torch's allocator, which keeps calls on different streams, and in captured
+        graphs, apart; none where none is needed."""
         key = (n_q_heads, n_picked, self.n_kv_heads, self.page_size, self.bounds is None)
         n = seqs._workspace.get(key)
         if n is None:
@@ -566,36 +569,55 @@ class PagedCache:
             if n == 0:
                 raise CkvError(EINVAL, self.lib.ckv_last_error(None).decode())
             seqs._workspace[key] = n
-        return self.torch.empty(n, dtype=self.torch.uint8, device=self.device) if n > least else None, n
+        if n <= 256:
+            return None, None, n
+        work = self._like.new_empty((n + 1) >> 1)
+        return work, work.data_ptr(), n
 
     def _rows(self, seqs, k, v, rows, first, starts):
         t = self.torch
-        for x in (k, v):
-            if x.dtype != t.bfloat16 or x.shape != k.shape or x.stride() != k.stride() or x.stride(-1) != 1:
-                raise CkvError(EINVAL, "rows must be two alike bf16 tensors with contiguous rows")
-        self._same_device(k, v, first, starts)
-        for x, n in ((first, seqs.batch), (starts, seqs.batch + 1)):
-            if x is not None and (x.dtype != t.int32 or x.shape != (n,) or not x.is_contiguous()):
-                raise CkvError(EINVAL, "first must be int32 [batch], starts int32 [batch + 1]")
-        packed = starts is not None
-        if packed and rows is None:
-            raise CkvError(EINVAL, "packed rows need `rows`, the most that one sequence has")
-        if not packed and k.dim() == 3:
-            k, v = k.unsqueeze(1), v.unsqueeze(1)
-        if not packed and rows is None:
-            rows = k.shape[1]
-        shape = (k.shape[0], self.n_kv_heads, self.head_dim) if packed else (seqs.batch, rows, self.n_kv_heads, self.head_dim)
-        if k.shape != shape:
-            raise CkvError(EINVAL, f"rows of shape {tuple(k.shape)}, {tuple(shape)} expected")
-        d = self.head_dim
-        return Rows(k.data_ptr(), v.data_ptr(), first.data_ptr() if first is not None else None, starts.data_ptr() if packed else None,
-                    0 if packed else _stride(k, 0, d), _stride(k, -3, d), _stride(k, -2, d), int(rows), k.shape[0] if packed else 0)
+        shape, stride = k.shape, k.stride()
+        if k.dtype is not t.bfloat16 or v.dtype is not t.bfloat16 or v.shape != shape or v.stride() != stride or stride[-1:] != (1,):
+            raise CkvError(EINVAL, "rows must be two alike bf16 tensors with contiguous rows")
+        if k.device != self.device or v.device != self.device:
+            self._same_device(k, v)
+        at_first = at_starts = None
+        if first is not None:
+            at_first = self._numbers(first, seqs.batch, "first must be int32 [batch], contiguous")
+        d, hkv = self.head_dim, self.n_kv_heads
+        if starts is not None:
+            at_starts = self._numbers(starts, seqs.batch + 1, "starts must be int32 [batch + 1], contiguous")
+            if rows is None:
+                raise CkvError(EINVAL, "packed rows need `rows`, the most that one sequence has")
+            if len(shape) != 3 or shape[1] != hkv or shape[2] != d:
+                raise CkvError(EINVAL, f"rows of shape {tuple(shape)}, [total][{hkv}][{d}] expected")
+            total, row_stride, head_stride = shape[0], stride[0], stride[1]
+            return Rows(k.data_ptr(), v.data_ptr(), at_first, at_starts, 0, row_stride if total > 1 else d, head_stride if hkv > 1 else d, rows, total)
+        if len(shape) == 3:
+            (batch, heads, width), count, (seq_stride, head_stride, _), row_stride = shape, 1, stride, d
+        elif len(shape) == 4:
+            (batch, count, heads, width), (seq_stride, row_stride, head_stride, _) = shape, stride
+        else:
+            batch = count = heads = width = 0
+        if batch != seqs.batch or heads != hkv or width != d or (rows is not None and rows != count):
+            raise CkvError(EINVAL, f"rows of shape {tuple(shape)}, [{seqs.batch}][{'rows' if rows is None else rows}][{hkv}][{d}] expected")
+        return Rows(k.data_ptr(), v.data_ptr(), at_first, None, seq_stride if batch > 1 else d, row_stride if count > 1 else d, head_stride if hkv > 1 else d, count, 0)
+
+    def _numbers(self, x, n, what):
+        """Address of an int32 array of n."""
+        if x.dtype is not self.torch.int32 or x.shape != (n,) or not x.is_contiguous():
+            raise CkvError(EINVAL, what)
+        if x.device != self.device:
+            self._same_device(x)
+        return x.data_ptr()
 
     def _query(self, seqs, q):
-        if q.dtype != self.torch.bfloat16 or q.dim() != 3 or q.shape[0] != seqs.batch or q.shape[2] != self.head_dim or q.stride(2) != 1:
+        shape, stride = q.shape, q.stride()
+        if q.dtype is not self.torch.bfloat16 or len(shape) != 3 or shape[0] != seqs.batch or shape[2] != self.head_dim or stride[2] != 1:
             raise CkvError(EINVAL, "q must be bf16 [batch][n_q_heads][128] with contiguous rows")
-        self._same_device(q)
-        return Query(q.data_ptr(), _stride(q, 0, self.head_dim), _stride(q, 1, self.head_dim), q.shape[1])
+        if q.device != self.device:
+            self._same_device(q)
+        return Query(q.data_ptr(), stride[0] if shape[0] > 1 else self.head_dim, stride[1] if shape[1] > 1 else self.head_dim, shape[1])
 
     # ------------------------------------------------------------------ calls
     def sequences(self, table, lengths, max_length=None):
@@ -618,7 +640,8 @@ class PagedCache:
             if starts is not None and total is None:
                 raise CkvError(EINVAL, "packed rows need `total` or `out`")
             shape = (seqs.batch, int(rows)) if starts is None else (int(total),)
-            out = tuple(t.empty((*shape, self.n_kv_heads, self.head_dim), dtype=t.bfloat16, device=self.device) for _ in range(2))
+            shape += (self.n_kv_heads, self.head_dim)
+            out = self._like.new_empty(shape), self._like.new_empty(shape)
         r = self._rows(seqs, *out, rows, first, starts)
         self._call(self.lib.ckv_paged_read, self._ref, seqs._ref, C.addressof(r))
         return out
@@ -636,14 +659,14 @@ class PagedCache:
             n_picked = pages.shape[2]
         dtype = t.float32 if f32 else t.bfloat16
         if out is None:
-            out = t.empty(q.shape, dtype=dtype, device=self.device)
+            out = t.empty_like(q, dtype=dtype) if q.is_contiguous() else t.empty(q.shape, dtype=dtype, device=self.device)
         elif out.dtype != dtype or out.shape != q.shape or not out.is_contiguous() or out.device != self.device:
             raise CkvError(EINVAL, f"out must be a contiguous {dtype} tensor of q's shape")
         sums = t.empty(q.shape[:2], dtype=t.float32, device=self.device) if lse else None
-        work, n = self._workspace(seqs, q.shape[1], n_picked)
+        work, at, n = self._workspace(seqs, q.shape[1], n_picked)
         self._call(self.lib.ckv_paged_attend, self._ref, seqs._ref, C.addressof(query), self._scale if scale is None else scale,
                    pages.data_ptr() if pages is not None else None, n_picked, out.data_ptr(), F32 if f32 else BF16, sums.data_ptr() if lse else None,
-                   work.data_ptr() if work is not None else None, n)
+                   at, n)
         return out, sums
 
     def select(self, seqs, q, keep, *, first=1, last=1, out=None):
@@ -653,12 +676,11 @@ class PagedCache:
         query = self._query(seqs, q)
         shape = (seqs.batch, self.n_kv_heads, int(keep))
         if out is None:
-            out = t.empty(shape, dtype=t.int32, device=self.device)
+            out = self._status.new_empty(shape)
         elif out.dtype != t.int32 or out.shape != shape or not out.is_contiguous() or out.device != self.device:
             raise CkvError(EINVAL, "out must be a contiguous int32 tensor [batch][n_kv_heads][keep]")
-        work, n = self._workspace(seqs, q.shape[1], 0, 0)
-        self._call(self.lib.ckv_paged_select, self._ref, seqs._ref, C.addressof(query), int(keep), int(first), int(last), out.data_ptr(),
-                   work.data_ptr() if work is not None else None, n)
+        work, at, n = self._workspace(seqs, q.shape[1], -1)
+        self._call(self.lib.ckv_paged_select, self._ref, seqs._ref, C.addressof(query), int(keep), int(first), int(last), out.data_ptr(), at, n)
         return out
 
     def status(self):

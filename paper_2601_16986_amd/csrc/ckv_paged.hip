@@ -156,7 +156,10 @@ Split split_of(const ckv_pages* p, const ckv_seqs* s, int n_q_heads, int n_picke
   return r;
 }
 int score_columns(const ckv_pages* p, const ckv_seqs* s) { return (int)(((long long)s->max_length + p->page_size - 1) / p->page_size); }
-size_t score_bytes(const ckv_pages* p, const ckv_seqs* s) { return up256((size_t)s->batch * p->n_kv_heads * score_columns(p, s) * 4); }
+size_t score_bytes(const ckv_pages* p, const ckv_seqs* s, int n_cu) {
+  const int units = s->batch * p->n_kv_heads, columns = score_columns(p, s);
+  return selects_whole(units, columns, n_cu) ? 0 : up256((size_t)units * columns * 4);
+}
 
 }  // namespace
 
@@ -201,9 +204,9 @@ int ckv_paged_read(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_rows*
 size_t ckv_paged_workspace_bytes(const ckv_pages* pages, const ckv_seqs* seqs, int32_t n_q_heads, int32_t n_picked) {
   if (check(pages, seqs) != CKV_OK) return 0;
   if (n_q_heads < pages->n_kv_heads || n_q_heads % pages->n_kv_heads != 0 || n_q_heads / pages->n_kv_heads > kPagedGroup) return 0;
+  if (n_picked == -1) return std::max<size_t>(256, score_bytes(pages, seqs, compute_units()));
   if (n_picked < 0 || (long long)n_picked * pages->page_size > kMaxLength || too_many(pages, seqs, n_picked)) return 0;
-  const Split s = split_of(pages, seqs, n_q_heads, n_picked, compute_units());
-  return std::max<size_t>(256, std::max(s.bytes(), pages->bounds ? score_bytes(pages, seqs) : 0));
+  return std::max<size_t>(256, split_of(pages, seqs, n_q_heads, n_picked, compute_units()).bytes());
 }
 
 int ckv_paged_attend(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_query* query, float softmax_scale, const int32_t* picked, int32_t n_picked, void* out,
@@ -286,7 +289,7 @@ int ckv_paged_select(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_que
     return launched("ckv_paged_select");
   }
   if (columns > keep) {
-    if (!workspace || !aligned(workspace, 256) || workspace_bytes < score_bytes(pages, seqs)) return fail(CKV_EWORKSPACE, "workspace too small or misaligned");
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < score_bytes(pages, seqs, n_cu)) return fail(CKV_EWORKSPACE, "workspace too small or misaligned");
     const int each = score_pages_each((int)units, columns, n_cu);
     const dim3 grid(units, (unsigned)((columns + each - 1) / each));
     auto score = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, (hipStream_t)stream, p, c, each); };

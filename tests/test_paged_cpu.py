@@ -206,7 +206,7 @@ def test_other_arguments_that_are_refused(good):
     assert {select(work=None), select(size=1024), select(work=4352 + 8)} == {ckv.EWORKSPACE}
     for args in ((None, s, r), (p, None, r), (p, s, None)):
         assert lib.ckv_paged_append(*args, None) == ckv.EINVAL and lib.ckv_paged_read(*args, None) == ckv.EINVAL
-    assert lib.ckv_paged_workspace_bytes(p, s, 7, 0) == 0 and lib.ckv_paged_workspace_bytes(p, s, 8, -1) == 0
+    assert lib.ckv_paged_workspace_bytes(p, s, 7, 0) == 0 and lib.ckv_paged_workspace_bytes(p, s, 8, -2) == 0 and lib.ckv_paged_workspace_bytes(p, s, 8, -1) == 4 * 6 * 32768
 
 
 def test_pools_of_the_binding_that_are_refused():
