@@ -477,7 +477,7 @@ class PagedSequences:
         cache._same_device(table, lengths)
         self.batch, self.columns = table.shape
         self.max_length = int(max_length) if max_length is not None else self.columns * cache.page_size
-        self.table, self.lengths = table, lengths
+        self.table, self.lengths, self.device = table, lengths, cache.device
         self._struct = Seqs(table.data_ptr(), lengths.data_ptr(), _stride(table, 0, self.columns), self.batch, self.columns, self.max_length)
         self._ref = C.addressof(self._struct)
         self._workspace = {}
@@ -545,7 +545,7 @@ class PagedCache:
     def _same_device(self, *tensors):
         for x in tensors:
             if x is not None and x.device != self.device:
-                raise CkvError(EINVAL, f"a tensor on {x.device} with a cache on {self.device}")
+                raise CkvError(EINVAL, f"{'sequences' if isinstance(x, PagedSequences) else 'a tensor'} on {x.device} with a cache on {self.device}")
 
     def _call(self, entry, *args):
         """entry(*args, stream) on the pools' device."""
@@ -579,8 +579,8 @@ class PagedCache:
         shape, stride = k.shape, k.stride()
         if k.dtype is not t.bfloat16 or v.dtype is not t.bfloat16 or v.shape != shape or v.stride() != stride or stride[-1:] != (1,):
             raise CkvError(EINVAL, "rows must be two alike bf16 tensors with contiguous rows")
-        if k.device != self.device or v.device != self.device:
-            self._same_device(k, v)
+        if k.device != self.device or v.device != self.device or seqs.device != self.device:
+            self._same_device(k, v, seqs)
         at_first = at_starts = None
         if first is not None:
             at_first = self._numbers(first, seqs.batch, "first must be int32 [batch], contiguous")
@@ -615,8 +615,8 @@ class PagedCache:
         shape, stride = q.shape, q.stride()
         if q.dtype is not self.torch.bfloat16 or len(shape) != 3 or shape[0] != seqs.batch or shape[2] != self.head_dim or stride[2] != 1:
             raise CkvError(EINVAL, "q must be bf16 [batch][n_q_heads][128] with contiguous rows")
-        if q.device != self.device:
-            self._same_device(q)
+        if q.device != self.device or seqs.device != self.device:
+            self._same_device(q, seqs)
         return Query(q.data_ptr(), stride[0] if shape[0] > 1 else self.head_dim, stride[1] if shape[1] > 1 else self.head_dim, shape[1])
 
     # ------------------------------------------------------------------ calls

@@ -76,9 +76,10 @@ CKV_PLAN AttendPlan attend_plan(long long units, int entries, bool same, int n_c
   return {0, 0, workers, workers + units, true};
 }
 
-// Whether a selection is one kernel, a workgroup per unit, or two: scores by workgroups of so many pages, then the picking.
+// Whether a selection is one kernel, a workgroup per unit, or two: scores by workgroups of so many pages, then the picking.  us, one kernel / two: 8 units of 256 pages 8.6 /
+// 8.3, 64 of 293 14.3 / 14.0, 64 of 512 14.7 / 13.1, 8 of 512 11.5 / 8.5, 512 of 293 14.6 / 16.3, 512 of 512 28.6 / 42; a second launch takes the host 3 us more.
 constexpr int kFewPages = 512;
-CKV_PLAN bool selects_whole(int units, int columns, int n_cu) { return columns <= (units >= n_cu ? kFewPages : kFewPages / 2); }
+CKV_PLAN bool selects_whole(int units, int columns, int n_cu) { return columns <= (units >= n_cu ? kFewPages : kFewPages * 5 / 8); }
 // Whether a selection reads bounds past the caches: not where those of several layers stay in the last one (256 MiB).  us, through / past: 64 sequences of 8 heads, 256
 // pages each (67 MB) 16.4 / 17.7, 512 (134 MB) 32.8 / 28.6, 1000 (262 MB) 63 / 54.
 CKV_PLAN bool bounds_past_caches(long long units, int columns) { return units * columns * 4 * kDim >= (96ll << 20); }

@@ -96,9 +96,13 @@ Paged paged_of(const ckv_pages* p, const ckv_seqs* s) {
   return d;
 }
 
-int check_rows(const ckv_pages* p, const ckv_rows* r) {
-  (void)p;
-  if (!r || !r->k || !r->v) return fail(CKV_EINVAL, "rows are NULL");
+// Packed rows of which there are none.
+bool nothing(const ckv_rows* r) { return r->starts && r->total == 0; }
+
+int check_rows(const ckv_rows* r) {
+  if (!r) return fail(CKV_EINVAL, "rows are NULL");
+  if (nothing(r)) return CKV_OK;
+  if (!r->k || !r->v) return fail(CKV_EINVAL, "rows are NULL");
   if (!aligned(r->k, 16) || !aligned(r->v, 16)) return fail(CKV_EINVAL, "rows must be 16-byte aligned");
   if (r->rows < 1 || r->rows > kMaxLength) return fail(CKV_EINVAL, "rows must be in [1, 2^30]");
   if (!stride_ok(r->row_stride, kDim, 8) || !stride_ok(r->head_stride, kDim, 8) || (r->starts ? r->total < 0 : !stride_ok(r->seq_stride, kDim, 8)))
@@ -171,8 +175,8 @@ extern "C" {
 
 int ckv_paged_append(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_rows* rows, void* stream) {
   if (int rc = check(pages, seqs)) return rc;
-  if (int rc = check_rows(pages, rows)) return rc;
-  if (seqs->max_length == 0) return CKV_OK;
+  if (int rc = check_rows(rows)) return rc;
+  if (seqs->max_length == 0 || nothing(rows)) return CKV_OK;
   const Paged p = paged_of(pages, seqs);
   const Rows r = rows_of(rows);
   const long long reach = std::min<long long>(rows->rows, seqs->max_length), touched = std::min<long long>((reach + pages->page_size - 2) / pages->page_size + 1, seqs->columns);
@@ -187,8 +191,8 @@ int ckv_paged_append(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_row
 
 int ckv_paged_read(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_rows* rows, void* stream) {
   if (int rc = check(pages, seqs)) return rc;
-  if (int rc = check_rows(pages, rows)) return rc;
-  if (seqs->max_length == 0) return CKV_OK;
+  if (int rc = check_rows(rows)) return rc;
+  if (seqs->max_length == 0 || nothing(rows)) return CKV_OK;
   const Paged p = paged_of(pages, seqs);
   const Rows r = rows_of(rows);
   const long long pieces = (std::min<long long>(rows->rows, seqs->max_length) + kReadRows - 1) / kReadRows;

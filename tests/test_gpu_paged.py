@@ -180,7 +180,7 @@ def test_attention_over_lengths(e4m3, ps, layout, lengths):
     assert none is None and torch.equal(out, again), "the same call, the same bits"
 
 
-@pytest.mark.parametrize("batch,length,hkv", [(1, 40000, 1), (300, 130, 2), (3, 9000, 8)])
+@pytest.mark.parametrize("batch,length,hkv", [(1, 40000, 1), (300, 130, 2), (3, 9000, 8), (64, 3000, 1), (65, 3000, 1), (130, 2100, 2), (300, 900, 1)])
 def test_attention_in_few_and_many_pieces(batch, length, hkv):
     """From one unit cut into pieces for the whole chip to more units than workgroups run at once."""
     rng = np.random.default_rng(batch)
@@ -191,6 +191,15 @@ def test_attention_in_few_and_many_pieces(batch, length, hkv):
     few = [b for b in range(batch) if b < 2 or b % 37 == 0]
     f.lengths, f.k, f.v = [f.lengths[b] for b in few], [f.k[b] for b in few], [f.v[b] for b in few]
     check_attention(f, q[few], out[few], lse[few])
+
+
+@pytest.mark.parametrize("e4m3", [True, False])
+@pytest.mark.parametrize("hq,f32", [(16, True), (11, False), (1, True)])
+def test_long_attention_of_other_groups(e4m3, hq, f32):
+    f = Filled([3333, 1, 6000], 1, 32, e4m3, seed=hq)
+    q = f.queries(hq)
+    out, lse = f.cache.attend(f.seqs, device(q), lse=True, f32=f32)
+    check_attention(f, q, out, lse)
 
 
 @pytest.mark.parametrize("e4m3", [True, False])
@@ -383,6 +392,22 @@ def test_wrong_tables_lengths_and_lists_are_reported_and_left_out():
     raw = h.cache.k.view(torch.uint8).clone()
     h.cache.append(h.seqs, *(torch.zeros((5, 1, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2)), rows=5, starts=torch.tensor([0, 6, 6, 4], dtype=torch.int32, device=DEV))
     assert h.cache.status() == ckv.BAD_LENGTH and torch.equal(raw, h.cache.k.view(torch.uint8))
+
+
+def test_calls_with_nothing_to_do():
+    f = Filled([20, 0], 2, 16, True)
+    none, starts = torch.zeros((0, 2, 128), dtype=torch.bfloat16, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV)
+    before = f.cache.k.view(torch.uint8).clone()
+    f.cache.append(f.seqs, none, none, rows=4, starts=starts)
+    k, v = f.cache.read(f.seqs, 4, starts=starts, total=0)
+    assert k.shape == v.shape == none.shape and torch.equal(before, f.cache.k.view(torch.uint8))
+    s = f.cache.sequences(f.seqs.table, torch.zeros_like(f.seqs.lengths), 0)
+    q = device(f.queries(4))
+    out, lse = f.cache.attend(s, q, lse=True)
+    assert (out == 0).all() and (lse == -float("inf")).all()
+    assert (f.cache.select(s, q, 3) == -1).all()
+    f.cache.append(s, torch.zeros((2, 2, 128), dtype=torch.bfloat16, device=DEV), torch.zeros((2, 2, 128), dtype=torch.bfloat16, device=DEV))
+    assert f.cache.status() == 0 and torch.equal(before, f.cache.k.view(torch.uint8))
 
 
 def test_refusals_of_the_binding():
