@@ -147,7 +147,10 @@ __device__ __forceinline__ u32x4 values8(u32x2 codes, float scale) {
 }
 
 // One workgroup per (sequence, KV head) and page that new rows reach: it alone touches the page's rows and extremes, so that these need no atomics.  Sixteen
-// lanes take a row, 16 bytes of bf16 each, for key and value.
+// lanes take a row, 16 bytes of bf16 each, for key and value.  Where rows are many it is bound by memory: 322208 rows (165 MB in, 83 MB out) 57 us, 4.3 TB/s, where a plain copy
+// reaches 4.7; magnitudes and codes from packed bf16 instead of floats were worth a fifth where the rows were in the caches (72192 rows 19.3 -> 16.1 us).  A single
+// row of each of 32 sequences, 8 heads, takes 4 us: four dependent trips to memory.  (Spans of 64 rows of smaller pages, all rows asked for at once, took
+// longer: 69 us, and 6 instead of 4 for a prompt of 777.)
 template <bool E4M3, int NT>
 __global__ __launch_bounds__(NT) void paged_append_kernel(Paged p, Rows r) {
   __shared__ float s_lo[NT / 64][kDim], s_hi[NT / 64][kDim];
@@ -223,7 +226,8 @@ __global__ __launch_bounds__(NT) void paged_append_kernel(Paged p, Rows r) {
   }
 }
 
-// Sixteen lanes take a row, 32 rows per workgroup, two of them asked for at once.  PAST: rows are stored past the caches (reads_past_caches).
+// Sixteen lanes take a row, 32 rows per workgroup, two of them asked for at once (64 rows, four at once: 60.4 us for 322208 rows that now take 49.9).  PAST: rows are
+// stored past the caches (reads_past_caches).
 constexpr int kReadRows = 32;
 template <bool E4M3, bool PAST>
 __global__ __launch_bounds__(kThreads) void paged_read_kernel(Paged p, Rows r) {
@@ -389,6 +393,11 @@ __device__ __forceinline__ bool find_piece(const Paged& p, const Attend& c, int 
 //           dimensions 8 j + dt), in the entry order in which K Q^T leaves the logits.
 // The weights are split into bf16 terms: high ones in rows 0 .. 7 and low ones in rows 8 .. 15 of one operand for up to eight heads (the queries are
 // there twice), as operands of their own for more (WIDE).  Two terms hold 16 bits of a weight; a float output gets a third.
+//
+// It is bound by memory: 64 sequences x 8 KV heads of 9350 entries in 8 bits, 1236 MB (1243 by the counters), 189 us, 6.5 TB/s of the 7.1 of a plain read, and the same
+// without any of the arithmetic, which keeps the vector units busy for a fifth of the time.  Eight wavefronts per compute unit are enough, and more, or blocks asked
+// for one ahead, only make the streams more: 12 .. 16 of them 202 .. 217 us, 8 KB instead of 4 KB in flight each 191.  A piece costs some 3 us beside its
+// entries (length, page, rows: three trips; joining four wavefronts), so pieces are as few as fill the chip: twice, four, eight times as many 202, 205, 208 us.
 template <bool E4M3, int TERMS, bool WIDE>
 __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend c) {
   constexpr int kHeads = WIDE ? 16 : 8, kWaves = kAttendWaves, kRow = kDim + 4, kParts = E4M3 ? 1 : 2;
@@ -626,7 +635,8 @@ __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend 
 }
 
 // Joins the pieces of units that have several: a workgroup takes `heads` query heads of a unit, eight / heads rows of 32 threads (four dimensions each) a head, a row eight
-// parts at a time.
+// parts at a time.  2.6 .. 4.7 us, of which a launch and three trips to memory are most.  (The last workgroup to arrive at a counter joining instead, with accesses past the
+// caches: the same times or 2 us more, and the counters would have to be zero before.)
 constexpr int kJoinRows = 8;
 __global__ __launch_bounds__(32 * kJoinRows) void paged_join_kernel(Attend c, int heads) {
   __shared__ float s_m[kJoinRows], s_l[kJoinRows];
@@ -693,7 +703,8 @@ struct Select {
 
 // A page's score is the sum over the group's heads of the largest logit that its extremes allow, sum_d max(q_d min_d, q_d max_d): with the heads'
 // positive and negative parts summed beforehand one product of 256 terms.  In 64 bits, because scores decide: whoever adds up in another order gets the same
-// pages.  Sixteen lanes take a page, 8 dimensions of both extremes each.
+// pages.  Sixteen lanes take a page, 8 dimensions of both extremes each; the arithmetic (16 products in 64 bits and a sum over the lanes) is a third of what the
+// memory allows.  512 units of 1000 pages (262 MB) 54 us with the picking; 8 of 2048 5.6 and 5.5, where the picking's rounds over the workgroup decide.
 struct Parts {
   double up[8], down[8];
 };
