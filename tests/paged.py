@@ -31,8 +31,10 @@ def pools(n_pages, hkv, ps, e4m3, layout="plain", bounds=True, poison=True):
             x.view(torch.uint8 if e4m3 else torch.int16).fill_(0x7F if e4m3 else 0x7FC0)
         return x
 
-    scales = torch.full((n_pages, hkv, ps, 2), 255, dtype=torch.uint8, device=DEV) if e4m3 else None
-    b = torch.full((n_pages, hkv, 2, 128), float("nan"), dtype=torch.bfloat16, device=DEV) if bounds else None
+    some = (lambda *shape: (shape[0], 3, *shape[1:])) if layout == "layers" else (lambda *shape: shape)
+    mine = (lambda x: x[:, 2]) if layout == "layers" else (lambda x: x)
+    scales = mine(torch.full(some(n_pages, hkv, ps, 2), 255, dtype=torch.uint8, device=DEV)) if e4m3 else None
+    b = mine(torch.full(some(n_pages, hkv, 2, 128), float("nan"), dtype=torch.bfloat16, device=DEV)) if bounds else None
     return ckv.PagedCache(rows(), rows(), scales=scales, bounds=b)
 
 

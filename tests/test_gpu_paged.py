@@ -318,6 +318,30 @@ def test_pages_are_picked_by_score(hq, hkv, lengths, ps, keep, first, last):
     assert f.cache.status() == 0
 
 
+@pytest.mark.parametrize("batch,hkv,columns", [(3, 2, 320), (3, 2, 321), (40, 8, 512), (40, 8, 513), (40, 8, 320), (2, 1, 1024), (2, 1, 1025), (1, 2, 4097), (1, 1, 8193), (1, 1, 32768), (64, 16, 513)])
+def test_picking_where_it_changes_its_way(batch, hkv, columns):
+    """Sequences of up to so many pages, all of one small pool in their own order, which bounds alone decide."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(columns)
+    pages, ps, heads = 700, 16, 2 * hkv
+    cache = pools(pages, hkv, ps, True)
+    lo, hi = (torch.randn((pages, hkv, 128), generator=g, device=DEV).bfloat16() for _ in range(2))
+    cache.bounds[:, :, 0], cache.bounds[:, :, 1] = torch.minimum(lo, hi), torch.maximum(lo, hi)
+    table = torch.randint(0, pages, (batch, columns), generator=g, device=DEV).int()
+    rng = np.random.default_rng(columns)
+    lengths = [columns * ps - 3] + [int(x) for x in rng.integers(1, columns * ps + 1, batch - 1)]
+    q = torch.randn((batch, heads, 128), generator=g, device=DEV).bfloat16()
+    keep = 29
+    got = cache.select(cache.sequences(table, torch.tensor(lengths, dtype=torch.int32, device=DEV)), q, keep).cpu().numpy()
+    bounds, t, qd = cache.bounds.double().cpu().numpy(), table.cpu().numpy(), q.double().cpu().numpy()
+    for b in range(min(batch, 12)):
+        held = -(-lengths[b] // ps)
+        for h in range(hkv):
+            each = ref.scores(qd[b, 2 * h:2 * h + 2], bounds[:, h, 0], bounds[:, h, 1])        # of the pool's pages; a sequence has some of them again and again: ties
+            assert got[b, h].tolist() == ref.pick(each[t[b, :held]], keep, 1, 1).tolist(), f"sequence {b} head {h}"
+    assert cache.status() == 0
+
+
 def test_pages_of_equal_and_of_no_score():
     """Ties go to the lowest page, what is no number comes first, infinities where they belong."""
     f = Filled([16 * 40], 1, 16, False, seed=1)
