@@ -301,7 +301,8 @@ int ckv_paged_select(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_que
     if (int rc = launched("ckv_paged_select")) return rc;
   }
   auto pick = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(units), dim3((unsigned)threads), 0, (hipStream_t)stream, p, c); };
-  if (columns <= 4 * kThreads) pick(paged_pick_kernel<4, kThreads>, kThreads);
+  if (columns <= 2 * kPickThreads) pick(paged_pick_kernel<2, kPickThreads>, kPickThreads);
+  else if (columns <= 4 * kPickThreads) pick(paged_pick_kernel<4, kPickThreads>, kPickThreads);
   else if (columns <= 4 * kWideThreads) pick(paged_pick_kernel<4, kWideThreads>, kWideThreads);
   else if (columns <= 8 * kWideThreads) pick(paged_pick_kernel<8, kWideThreads>, kWideThreads);
   else pick(paged_pick_kernel<32, kWideThreads>, kWideThreads);

@@ -704,7 +704,7 @@ struct Select {
 // A page's score is the sum over the group's heads of the largest logit that its extremes allow, sum_d max(q_d min_d, q_d max_d): with the heads'
 // positive and negative parts summed beforehand one product of 256 terms.  In 64 bits, because scores decide: whoever adds up in another order gets the same
 // pages.  Sixteen lanes take a page, 8 dimensions of both extremes each; the arithmetic (16 products in 64 bits and a sum over the lanes) is a third of what the
-// memory allows.  512 units of 1000 pages (262 MB) 54 us with the picking; 8 of 2048 5.6 and 5.5, where the picking's rounds over the workgroup decide.
+// memory allows.  512 units of 1000 pages (262 MB) 54 us with the picking; 8 of 2048 5.6 and 4.9, where the picking's rounds over the workgroup decide (512 threads; 256 or 1024 0.6 longer).
 struct Parts {
   double up[8], down[8];
 };
