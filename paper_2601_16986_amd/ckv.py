@@ -528,7 +528,10 @@ class PagedCache:
                              k.stride(2), *s, *b, k.data_ptr(), v.data_ptr(), scales.data_ptr() if scales is not None else None,
                              bounds.data_ptr() if bounds is not None else None, self._status.data_ptr())
         self._ref = C.addressof(self._struct)
+        # what every call looks up, looked up once
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self._current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        self._bf16, self._f32, self._geometry = torch.bfloat16, torch.float32, (self.n_kv_heads, self.page_size, bounds is None)
         self._scale = 1.0 / float(np.sqrt(self.head_dim))
 
     @classmethod
@@ -550,7 +553,7 @@ class PagedCache:
     def _call(self, entry, *args):
         """entry(*args, stream) on the pools' device."""
         index = self._index
-        if self._raw_stream is not None and self.torch.cuda.current_device() == index:
+        if self._raw_stream is not None and self._current_device() == index:
             rc = entry(*args, self._raw_stream(index))
         else:
             with self.torch.cuda.device(self.device):
@@ -561,7 +564,7 @@ class PagedCache:
     def _workspace(self, seqs, n_q_heads, n_picked):
         """(tensor, address, bytes) of a workspace for a call of these sizes, from torch's allocator, which keeps calls on different streams, and in captured
         graphs, apart; none where none is needed."""
-        key = (n_q_heads, n_picked, self.n_kv_heads, self.page_size, self.bounds is None)
+        key = (n_q_heads, n_picked, self._geometry)
         n = seqs._workspace.get(key)
         if n is None:
             with self.torch.cuda.device(self.device):
@@ -575,18 +578,17 @@ class PagedCache:
         return work, work.data_ptr(), n
 
     def _rows(self, seqs, k, v, rows, first, starts):
-        t = self.torch
-        shape, stride = k.shape, k.stride()
-        if k.dtype is not t.bfloat16 or v.dtype is not t.bfloat16 or v.shape != shape or v.stride() != stride or stride[-1:] != (1,):
+        shape, stride, bf16 = k.shape, k.stride(), self._bf16
+        if k.dtype is not bf16 or v.dtype is not bf16 or v.shape != shape or v.stride() != stride or stride[-1:] != (1,):
             raise CkvError(EINVAL, "rows must be two alike bf16 tensors with contiguous rows")
         if k.device != self.device or v.device != self.device or seqs.device != self.device:
             self._same_device(k, v, seqs)
         at_first = at_starts = None
         if first is not None:
-            at_first = self._numbers(first, seqs.batch, "first must be int32 [batch], contiguous")
+            at_first = self._numbers(first, (seqs.batch,), "first must be int32 [batch], contiguous")
         d, hkv = self.head_dim, self.n_kv_heads
         if starts is not None:
-            at_starts = self._numbers(starts, seqs.batch + 1, "starts must be int32 [batch + 1], contiguous")
+            at_starts = self._numbers(starts, (seqs.batch + 1,), "starts must be int32 [batch + 1], contiguous")
             if rows is None:
                 raise CkvError(EINVAL, "packed rows need `rows`, the most that one sequence has")
             if len(shape) != 3 or shape[1] != hkv or shape[2] != d:
@@ -603,9 +605,9 @@ class PagedCache:
             raise CkvError(EINVAL, f"rows of shape {tuple(shape)}, [{seqs.batch}][{'rows' if rows is None else rows}][{hkv}][{d}] expected")
         return Rows(k.data_ptr(), v.data_ptr(), at_first, None, seq_stride if batch > 1 else d, row_stride if count > 1 else d, head_stride if hkv > 1 else d, count, 0)
 
-    def _numbers(self, x, n, what):
-        """Address of an int32 array of n."""
-        if x.dtype is not self.torch.int32 or x.shape != (n,) or not x.is_contiguous():
+    def _numbers(self, x, shape, what):
+        """Address of a contiguous int32 array of that shape."""
+        if x.dtype is not self.torch.int32 or x.shape != shape or not x.is_contiguous():
             raise CkvError(EINVAL, what)
         if x.device != self.device:
             self._same_device(x)
@@ -613,11 +615,11 @@ class PagedCache:
 
     def _query(self, seqs, q):
         shape, stride = q.shape, q.stride()
-        if q.dtype is not self.torch.bfloat16 or len(shape) != 3 or shape[0] != seqs.batch or shape[2] != self.head_dim or stride[2] != 1:
+        if q.dtype is not self._bf16 or len(shape) != 3 or shape[0] != seqs.batch or shape[2] != self.head_dim or stride[2] != 1:
             raise CkvError(EINVAL, "q must be bf16 [batch][n_q_heads][128] with contiguous rows")
         if q.device != self.device or seqs.device != self.device:
             self._same_device(q, seqs)
-        return Query(q.data_ptr(), stride[0] if shape[0] > 1 else self.head_dim, stride[1] if shape[1] > 1 else self.head_dim, shape[1])
+        return shape, Query(q.data_ptr(), stride[0] if shape[0] > 1 else self.head_dim, stride[1] if shape[1] > 1 else self.head_dim, shape[1])
 
     # ------------------------------------------------------------------ calls
     def sequences(self, table, lengths, max_length=None):
@@ -635,7 +637,6 @@ class PagedCache:
 
     def read(self, seqs, rows, *, first=None, starts=None, total=None, out=None):
         """The same rows back, bf16: (k, v), new tensors (uninitialised behind a sequence's last row) or `out`."""
-        t = self.torch
         if out is None:
             if starts is not None and total is None:
                 raise CkvError(EINVAL, "packed rows need `total` or `out`")
@@ -649,37 +650,34 @@ class PagedCache:
     def attend(self, seqs, q, *, pages=None, scale=None, f32=False, lse=False, out=None):
         """Attention of one token per sequence, q bf16 [batch][n_q_heads][128]: (out, lse), out of q's shape in bf16 or float (f32), lse float
         [batch][n_q_heads] or None.  pages: int32 [batch][n_kv_heads][n], as select returns it: only their entries take part."""
-        t = self.torch
-        query = self._query(seqs, q)
-        n_picked = 0
+        shape, query = self._query(seqs, q)
+        at_pages, n_picked = None, 0
         if pages is not None:
-            if pages.dtype != t.int32 or pages.dim() != 3 or pages.shape[:2] != (seqs.batch, self.n_kv_heads) or pages.shape[2] < 1 or not pages.is_contiguous():
+            n_picked = pages.shape[-1]
+            if pages.shape != (seqs.batch, self.n_kv_heads, n_picked) or n_picked < 1:
                 raise CkvError(EINVAL, "pages must be int32 [batch][n_kv_heads][n], n at least 1, contiguous")
-            self._same_device(pages)
-            n_picked = pages.shape[2]
-        dtype = t.float32 if f32 else t.bfloat16
+            at_pages = self._numbers(pages, pages.shape, "pages must be int32 [batch][n_kv_heads][n], n at least 1, contiguous")
+        dtype = self._f32 if f32 else self._bf16
         if out is None:
-            out = t.empty_like(q, dtype=dtype) if q.is_contiguous() else t.empty(q.shape, dtype=dtype, device=self.device)
-        elif out.dtype != dtype or out.shape != q.shape or not out.is_contiguous() or out.device != self.device:
+            out = self.torch.empty_like(q, dtype=dtype) if q.is_contiguous() else self._like.new_empty(shape, dtype=dtype)
+        elif out.dtype is not dtype or out.shape != shape or not out.is_contiguous() or out.device != self.device:
             raise CkvError(EINVAL, f"out must be a contiguous {dtype} tensor of q's shape")
-        sums = t.empty(q.shape[:2], dtype=t.float32, device=self.device) if lse else None
-        work, at, n = self._workspace(seqs, q.shape[1], n_picked)
-        self._call(self.lib.ckv_paged_attend, self._ref, seqs._ref, C.addressof(query), self._scale if scale is None else scale,
-                   pages.data_ptr() if pages is not None else None, n_picked, out.data_ptr(), F32 if f32 else BF16, sums.data_ptr() if lse else None,
-                   at, n)
+        sums = self._like.new_empty(shape[:2], dtype=self._f32) if lse else None
+        work, at, n = self._workspace(seqs, shape[1], n_picked)
+        self._call(self.lib.ckv_paged_attend, self._ref, seqs._ref, C.addressof(query), self._scale if scale is None else scale, at_pages, n_picked, out.data_ptr(),
+                   F32 if f32 else BF16, sums.data_ptr() if lse else None, at, n)
         return out, sums
 
     def select(self, seqs, q, keep, *, first=1, last=1, out=None):
         """`keep` pages per sequence and KV head for q: the `first` first, the `last` last, the others by score; int32 [batch][n_kv_heads][keep], ascending,
         -1 behind the last."""
-        t = self.torch
-        query = self._query(seqs, q)
+        q_shape, query = self._query(seqs, q)
         shape = (seqs.batch, self.n_kv_heads, int(keep))
         if out is None:
             out = self._status.new_empty(shape)
-        elif out.dtype != t.int32 or out.shape != shape or not out.is_contiguous() or out.device != self.device:
-            raise CkvError(EINVAL, "out must be a contiguous int32 tensor [batch][n_kv_heads][keep]")
-        work, at, n = self._workspace(seqs, q.shape[1], -1)
+        else:
+            self._numbers(out, shape, "out must be a contiguous int32 tensor [batch][n_kv_heads][keep]")
+        work, at, n = self._workspace(seqs, q_shape[1], -1)
         self._call(self.lib.ckv_paged_select, self._ref, seqs._ref, C.addressof(query), int(keep), int(first), int(last), out.data_ptr(), at, n)
         return out
 
