@@ -472,7 +472,7 @@ __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend 
           vf[t][i] = stream16(vb + i * p.slot_stride + 16 * j);
         }
       }
-      if constexpr (E4M3) sc[t] = stream8(p.scales + pg * p.scale_page_stride + h * p.scale_head_stride + 2 * off + 8 * kg);
+      if constexpr (E4M3) sc[t] = load8(p.scales + pg * p.scale_page_stride + h * p.scale_head_stride + 2 * off + 8 * kg);      // (through the caches: a line serves several blocks)
     }
     // ---- logits of four entries of each tile
 #pragma unroll
