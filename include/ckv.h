@@ -436,10 +436,10 @@ typedef struct {
 
 /* Writes rows into their pages and brings the pages' bounds up to date (those of a page whose first slot is written start anew; writing a
  * position again leaves bounds that still hold, if wider than need be).  No two rows of a call may go to the same place: sequences of one call
- * must not share pages that it writes. */
+ * must not share pages that it writes.  The rows of one sequence may reach 65535 pages in a call (CKV_EINVAL otherwise). */
 int ckv_paged_append(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_rows* rows, void* stream);
 
-/* Reads rows back as bf16 (exact: see ckv_pages). */
+/* Reads rows back as bf16 (exact: see ckv_pages), up to 2^21 - 32 of a sequence in a call. */
 int ckv_paged_read(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_rows* rows, void* stream);
 
 /* Bytes of workspace that ckv_paged_attend needs (n_picked pages per KV head, 0: all entries), or ckv_paged_select (n_picked = -1), for these
@@ -451,7 +451,7 @@ size_t ckv_paged_workspace_bytes(const ckv_pages* pages, const ckv_seqs* seqs, i
  * exponentials, with which partial attentions can be joined.  A sequence without entries gets zeros and -inf; so does a head all of whose
  * logits are -inf.  With `picked` (dev [batch][n_kv_heads][n_picked], as ckv_paged_select leaves it) only the entries of the listed pages of the
  * sequence take part; -1 stands for no page, the order does not matter, and a page listed twice counts twice.  workspace: 256-byte aligned, NULL where
- * ckv_paged_workspace_bytes says 256.  Values of entries in use must be finite. */
+ * ckv_paged_workspace_bytes says 256.  Values of entries in use must be finite.  Entries of all sequences and KV heads together, by max_length: at most 2^35. */
 int ckv_paged_attend(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_query* query, float softmax_scale, const int32_t* picked,
                      int32_t n_picked, void* out, int32_t out_dtype, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
