@@ -448,7 +448,7 @@ size_t ckv_paged_workspace_bytes(const ckv_pages* pages, const ckv_seqs* seqs, i
 
 /* Attention of one new token per sequence (whose own row has been appended): out[b][g] = softmax(softmax_scale q K^T) V over the sequence's
  * entries, out dev out_dtype [batch][n_q_heads][128]; lse (dev float [batch][n_q_heads], or NULL) the natural logarithm of the sum of the
- * exponentials, with which partial attentions can be joined.  A sequence without entries gets zeros and -inf; so does a head all of whose
+ * exponentials, with which partial attentions can be joined.  Logits, weights and sums are held in float, whatever out_dtype.  A sequence without entries gets zeros and -inf; so does a head all of whose
  * logits are -inf.  With `picked` (dev [batch][n_kv_heads][n_picked], as ckv_paged_select leaves it) only the entries of the listed pages of the
  * sequence take part; -1 stands for no page, the order does not matter, and a page listed twice counts twice.  workspace: 256-byte aligned, NULL where
  * ckv_paged_workspace_bytes says 256.  Values of entries in use must be finite.  Entries of all sequences and KV heads together, by max_length: at most 2^35. */

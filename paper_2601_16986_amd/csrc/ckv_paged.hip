@@ -246,14 +246,9 @@ int ckv_paged_attend(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_que
   c.workers = s.plan.workers;
   const dim3 grid((unsigned)s.plan.pieces);
   auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, (hipStream_t)stream, p, c); };
-  const bool wide = G > 8, fine = out_dtype == CKV_F32;
-  if (pages->dtype == CKV_E4M3) {
-    if (wide) fine ? launch(paged_attend_kernel<true, 3, true>) : launch(paged_attend_kernel<true, 2, true>);
-    else fine ? launch(paged_attend_kernel<true, 3, false>) : launch(paged_attend_kernel<true, 2, false>);
-  } else {
-    if (wide) fine ? launch(paged_attend_kernel<false, 3, true>) : launch(paged_attend_kernel<false, 2, true>);
-    else fine ? launch(paged_attend_kernel<false, 3, false>) : launch(paged_attend_kernel<false, 2, false>);
-  }
+  const bool wide = G > 8;
+  if (pages->dtype == CKV_E4M3) wide ? launch(paged_attend_kernel<true, true>) : launch(paged_attend_kernel<true, false>);
+  else wide ? launch(paged_attend_kernel<false, true>) : launch(paged_attend_kernel<false, false>);
   if (int rc = launched("ckv_paged_attend")) return rc;
   if (!s.plan.split) return CKV_OK;
   const unsigned units = (unsigned)(seqs->batch * pages->n_kv_heads);

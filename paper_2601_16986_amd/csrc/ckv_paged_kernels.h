@@ -391,16 +391,17 @@ __device__ __forceinline__ bool find_piece(const Paged& p, const Attend& c, int 
 //           other dimensions than odd ones, so that each goes with both halves of the queries and half of the results are used;
 //   values  entries 4 kg .. 4 kg + 3, the eighth of the row at j: byte (or word) moves between pairs of entries make them operands of P V (columns =
 //           dimensions 8 j + dt), in the entry order in which K Q^T leaves the logits.
-// The weights are split into bf16 terms: high ones in rows 0 .. 7 and low ones in rows 8 .. 15 of one operand for up to eight heads (the queries are
-// there twice), as operands of their own for more (WIDE).  Two terms hold 16 bits of a weight; a float output gets a third.
+// The weights are split into three bf16 terms, which hold the 24 bits of a float: the high ones in rows 0 .. 7 and the second ones in rows 8 .. 15 of one operand for up to
+// eight heads (the queries are there twice), the third in another; operands of their own for more heads (WIDE).  (Two terms, 16
+// bits, whatever the output's type: 0.5 us less of 190, and outputs that nearly cancel off by 2^-18 of their terms.)
 //
 // It is bound by memory: 64 sequences x 8 KV heads of 9350 entries in 8 bits, 1236 MB (1243 by the counters), 189 us, 6.5 TB/s of the 7.1 of a plain read, and the same
 // without any of the arithmetic, which keeps the vector units busy for a fifth of the time.  Eight wavefronts per compute unit are enough, and more, or blocks asked
 // for one ahead, only make the streams more: 12 .. 16 of them 202 .. 217 us, 8 KB instead of 4 KB in flight each 191.  A piece costs some 3 us beside its
 // entries (length, page, rows: three trips; joining four wavefronts), so pieces are as few as fill the chip: twice, four, eight times as many 202, 205, 208 us.
-template <bool E4M3, int TERMS, bool WIDE>
+template <bool E4M3, bool WIDE>
 __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend c) {
-  constexpr int kHeads = WIDE ? 16 : 8, kWaves = kAttendWaves, kRow = kDim + 4, kParts = E4M3 ? 1 : 2;
+  constexpr int kHeads = WIDE ? 16 : 8, kTerms = 3, kWaves = kAttendWaves, kRow = kDim + 4, kParts = E4M3 ? 1 : 2;
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
   __shared__ __align__(16) float s_acc[kWaves][kHeads * kRow];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i32(tid >> 6), j = lane & 15, kg = lane >> 4, shift = p.shift;
@@ -535,26 +536,23 @@ __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend 
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[dt][i] *= f[i];
     }
-    bf16x8 w[3];
+    bf16x8 w[kTerms];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float weight = fast_exp2(sv[i] - m_run);
       l_run += weight;
       float rest = E4M3 ? weight * vs[i] : weight;
 #pragma unroll
-      for (int n = 0; n < TERMS; ++n) {
+      for (int n = 0; n < kTerms; ++n) {
         w[n][i] = (__bf16)rest;
         rest -= (float)w[n][i];
       }
     }
     if constexpr (!WIDE) {
       const bool low = j >= 8;
-      const u32x4 a = __builtin_bit_cast(u32x4, w[0]), z = __builtin_bit_cast(u32x4, w[1]);
+      const u32x4 a = __builtin_bit_cast(u32x4, w[0]), z = __builtin_bit_cast(u32x4, w[1]), y = __builtin_bit_cast(u32x4, w[2]);
       w[0] = __builtin_bit_cast(bf16x8, u32x4{low ? z[0] : a[0], low ? z[1] : a[1], low ? z[2] : a[2], low ? z[3] : a[3]});
-      if constexpr (TERMS == 3) {
-        const u32x4 y = __builtin_bit_cast(u32x4, w[2]);
-        w[1] = __builtin_bit_cast(bf16x8, u32x4{low ? 0u : y[0], low ? 0u : y[1], low ? 0u : y[2], low ? 0u : y[3]});
-      }
+      w[1] = __builtin_bit_cast(bf16x8, u32x4{low ? 0u : y[0], low ? 0u : y[1], low ? 0u : y[2], low ? 0u : y[3]});
     }
     // ---- weights times values: dimension 8 j + dt
 #pragma unroll
@@ -574,7 +572,7 @@ __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend 
         }
       }
 #pragma unroll
-      for (int n = 0; n < (WIDE ? TERMS : TERMS - 1); ++n)
+      for (int n = 0; n < (WIDE ? kTerms : kTerms - 1); ++n)
 #pragma unroll
         for (int i = 0; i < 2; ++i)
           acc[2 * d2 + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[n], __builtin_bit_cast(bf16x8, x[i]), acc[2 * d2 + i], 0, 0, 0);
