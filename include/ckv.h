@@ -412,10 +412,10 @@ typedef struct {
 } ckv_seqs;
 
 /* Rows in bf16 that a call writes into the cache or reads from it: of sequence b the positions first[b] .. (first: dev [batch];
- * NULL: lengths[b] - rows, or 0 if that is negative) up to lengths[b] - 1, at most `rows` of them.  Row i of sequence b and KV head h
+ * NULL: the sequence's last ones, as many as it has in the call, from position 0 if it is shorter) up to lengths[b] - 1, at most `rows` of them.  Row i of sequence b and KV head h
  * lies at b * seq_stride + i * row_stride + h * head_stride (in elements, multiples of 8), or, with starts (dev [batch + 1]:
- * sequences packed one after another), at (starts[b] + i) * row_stride + h * head_stride, and then there are at most
- * starts[b + 1] - starts[b] of them; `total` is the number of rows that k and v hold.  k, v 16-byte aligned.  Rows behind a
+ * sequences packed one after another), at (starts[b] + i) * row_stride + h * head_stride, and then the sequence has
+ * starts[b + 1] - starts[b] of them in the call (else `rows`); `total` is the number of rows that k and v hold.  k, v 16-byte aligned.  Rows behind a
  * sequence's last are not touched. */
 typedef struct {
   void* k;

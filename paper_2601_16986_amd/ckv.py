@@ -631,7 +631,8 @@ class PagedCache:
 
     def append(self, seqs, k, v, *, rows=None, first=None, starts=None):
         """Writes rows: k, v bf16 [batch][rows][n_kv_heads][128] (or [batch][n_kv_heads][128], one each), or with `starts` [total][n_kv_heads][128].
-        They become positions first .. lengths - 1 of their sequences (default: the last `rows`)."""
+        They become positions first .. lengths - 1 of their sequences (default: the last ones, as many as a sequence has in the call: `rows`, or with
+        `starts` its own number, at most `rows`)."""
         r = self._rows(seqs, k, v, rows, first, starts)
         self._call(self.lib.ckv_paged_append, self._ref, seqs._ref, C.addressof(r))
 

@@ -20,20 +20,20 @@ CKV_PLAN int page_fill(int length, int page, int shift) {
 // Whether a table's value names a page of the pool.
 CKV_PLAN bool page_there(int page, int n_pages) { return (unsigned)page < (unsigned)n_pages; }
 
-// Rows of one sequence in a call that writes or reads rows: positions first .. first + count - 1 of `length`.
+// Rows of one sequence in a call that writes or reads rows: positions first .. first + count - 1 of `length`; the last ones where the caller names no first, as many as
+// the sequence has in the call.
 struct RowSpan {
   int first, count;
   bool bad;
 };
 CKV_PLAN RowSpan row_span(int length, int most, bool has_first, int first, bool packed, int start, int stop, int total) {
-  if (!has_first) first = length > most ? length - most : 0;
-  if (first < 0 || first > length) return {0, 0, true};
-  int count = length - first < most ? length - first : most;
   if (packed) {
     if (start < 0 || stop < start || stop > total) return {0, 0, true};
-    if (stop - start < count) count = stop - start;
+    if (stop - start < most) most = stop - start;
   }
-  return {first, count, false};
+  if (!has_first) first = length > most ? length - most : 0;
+  if (first < 0 || first > length) return {0, 0, true};
+  return {first, length - first < most ? length - first : most, false};
 }
 
 // Whether a page's rows are written by one wavefront instead of four, where pages are enough to fill the chip all the same and have few new rows: the smallest

@@ -1,0 +1,29 @@
+"""The cache in pages without a GPU: which positions rows of a call go to, how an attention is cut, and what refusals say.  The
+index arithmetic is that of the kernels, compiled on its own."""
+from tests.test_paged_cpu import _run
+
+
+# ------------------------------------------------------------------ rows
+def test_rows_go_to_the_positions_that_the_header_names(tmp_path):
+    """Without `first` the last ones of the sequence, as many as it has in the call, packed or not."""
+    _run(tmp_path, r"""
+  const int total = 400;
+  for (int length : {0, 1, 5, 100, 300, 1 << 30})
+    for (int most : {1, 5, 10, 150, 300})
+      for (int has = 0; has < 2; ++has)
+        for (int first : {0, 1, 90, 97, 100})
+          for (int packed = 0; packed < 2; ++packed)
+            for (int start : {0, 7, 100})
+              for (int own : {0, 1, 3, 10, 200, 300}) {
+                const ckv::RowSpan s = ckv::row_span(length, most, has, first, packed, start, start + own, total);
+                const int there = packed && own < most ? own : most;
+                if (has && first > length) {
+                  if (!s.bad || s.count) return std::printf("rows behind the sequence\n"), 1;
+                  continue;
+                }
+                const int want = has ? first : length > there ? length - there : 0;
+                const int count = length - want < there ? length - want : there;
+                if (s.bad || s.count != count || (count && s.first != want)) return std::printf("length %d rows %d own %d: first %d count %d, %d %d expected\n", length, most, packed ? own : -1, s.first, s.count, want, count), 1;
+              }
+  const ckv::RowSpan s = ckv::row_span(100, 10, false, 0, true, 0, 3, 3);
+  if (s.first != 97 || s.count != 3 || s.bad) return std::printf("%d %d\n", s.first, s.count), 1;""")
