@@ -366,7 +366,8 @@ int ckv_bandwidth_probe(const void* src, void* dst, size_t bytes, void* sink, vo
  * without what is wrong and OR a bit into *status (if status is not NULL; the
  * library never clears it): */
 enum { CKV_PAGED_BAD_PAGE = 1,    /* a table entry that a sequence needs is not in [0, n_pages): its rows are neither read nor written */
-       CKV_PAGED_BAD_LENGTH = 2,  /* a length outside [0, max_length] (taken as the nearer of these), or rows that do not fit it (left out) */
+       CKV_PAGED_BAD_LENGTH = 2,  /* a length outside [0, max_length] (taken as the nearer of these; rows written or read
+                              * keep their positions, those from max_length on are left out), or rows that do not fit it (left out) */
        CKV_PAGED_BAD_PICK = 4 };  /* a picked page that the sequence does not have (left out) */
 
 /* The pools of one layer.  k, v: dev [n_pages][n_kv_heads][page_size][128] with

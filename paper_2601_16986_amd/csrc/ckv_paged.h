@@ -35,6 +35,12 @@ CKV_PLAN RowSpan row_span(int length, int most, bool has_first, int first, bool 
   if (first < 0 || first > length) return {0, 0, true};
   return {first, length - first < most ? length - first : most, false};
 }
+// Those below `limit`, the most that a length may be: of a sequence that outgrew it rows behind the limit are left out, none moves.
+CKV_PLAN RowSpan rows_below(RowSpan s, int limit) {
+  if (s.count > 0 && s.count > limit - s.first) s.count = limit - s.first;
+  if (s.count <= 0) s.first = s.count = 0;
+  return s;
+}
 
 // Whether a page's rows are written by one wavefront instead of four, where pages are enough to fill the chip all the same and have few new rows: the smallest
 // pages, or up to four rows a sequence (one pass either way). us, four / one: prompts of 8 x 9350 over 8 heads, pages of 16 80.7 / 63.3, of 32 62.6 / 63.5, of 64

@@ -75,10 +75,11 @@ struct Rows {
   int64_t seq_stride, row_stride, head_stride;     // bytes
   int32_t rows, total;
 
-  __device__ __forceinline__ RowSpan span(int b, int length, int64_t& base) const {
+  // rows of sequence b whose length the caller gives as `told`
+  __device__ __forceinline__ RowSpan span(int b, int told, int max_length, int64_t& base) const {
     const int start = starts ? starts[b] : 0, stop = starts ? starts[b + 1] : 0;
     base = starts ? start * row_stride : b * seq_stride;
-    return row_span(length, rows, first != nullptr, first ? first[b] : 0, starts != nullptr, start, stop, total);
+    return rows_below(row_span(told, rows, first != nullptr, first ? first[b] : 0, starts != nullptr, start, stop, total), max_length);
   }
 };
 
@@ -157,9 +158,9 @@ __global__ __launch_bounds__(NT) void paged_append_kernel(Paged p, Rows r) {
   const int u = blockIdx.x, b = u / p.hkv, h = u - b * p.hkv;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, piece = lane & 15, group = tid >> 4;
   int bad = 0;
-  const int length = p.length(b, bad);
+  p.length(b, bad);
   int64_t base;
-  const RowSpan span = r.span(b, length, base);
+  const RowSpan span = r.span(b, p.lengths[b], p.max_length, base);
   if (span.bad) bad |= PAGED_BAD_LENGTH;
   const int col = (span.first >> p.shift) + blockIdx.y;
   const int begin = max(span.first, col << p.shift), end = (int)min((int64_t)span.first + span.count, ((int64_t)col + 1) << p.shift);
@@ -233,9 +234,9 @@ template <bool E4M3, bool PAST>
 __global__ __launch_bounds__(kThreads) void paged_read_kernel(Paged p, Rows r) {
   const int u = blockIdx.x, b = u / p.hkv, h = u - b * p.hkv, piece = threadIdx.x & 15, group = threadIdx.x >> 4;
   int bad = 0;
-  const int length = uniform_i32(p.length(b, bad));
+  p.length(b, bad);
   int64_t base;
-  const RowSpan rows = r.span(b, length, base);
+  const RowSpan rows = r.span(b, uniform_i32(p.lengths[b]), p.max_length, base);
   if (rows.bad) bad |= PAGED_BAD_LENGTH;
   const int first = blockIdx.y * kReadRows;
   if (first >= rows.count) {

@@ -1,15 +1,22 @@
-"""Where the rows of a call go in a cache in pages: packed rows without their positions."""
+"""Where the rows of a call go in a cache in pages: packed rows without their positions, lengths beyond the most that the
+call was told."""
 import numpy as np
 import pytest
 import torch
 
 from tests.paged import DEV, Filled, bf16, device
+from paper_2601_16986_amd import ckv
 
 pytestmark = pytest.mark.gpu
 
 
 def _ints(x):
     return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def _raw(cache):
+    """Every byte that an append may write."""
+    return [x.view(torch.uint8).clone() for x in (cache.k, cache.v)] + [x.clone() for x in (cache.scales,) if x is not None] + [cache.bounds.view(torch.int16).clone()]
 
 
 def _check_rows(f, rows):
@@ -56,3 +63,48 @@ def test_packed_rows_of_more_than_a_sequence_holds():
         rows[side][0][:] = chunk[side][:6]
         rows[side][1][17:] = chunk[side][9:]
     _check_rows(f, rows)
+
+
+# ------------------------------------------------------------------ lengths beyond max_length
+@pytest.mark.parametrize("e4m3", [True, False])
+def test_rows_behind_the_largest_length_are_left_out(e4m3):
+    """A sequence that outgrew what the call was told: positions below the limit get their rows, the others' go nowhere, and no row moves."""
+    f = Filled([48, 30], 2, 16, e4m3, seed=5)
+    s = f.cache.sequences(f.seqs.table, f.seqs.lengths, 48)
+    one = [bf16(f.rng.standard_normal((2, 2, 128))) for _ in range(2)]
+    before = _raw(f.cache)
+    for far in (49, 60, 10 ** 9, 2 ** 31 - 1):
+        f.seqs.lengths.copy_(_ints([far, 0]))
+        f.cache.append(s, *(device(x) for x in one))
+        assert f.cache.status() == ckv.BAD_LENGTH
+        assert all(torch.equal(a, b) for a, b in zip(_raw(f.cache), before)), far
+        f.cache.append(s, *(device(x)[:1] for x in one), rows=1, starts=_ints([0, 1, 1]))
+        assert f.cache.status() == ckv.BAD_LENGTH
+        assert all(torch.equal(a, b) for a, b in zip(_raw(f.cache), before)), far
+        f.cache.append(s, *(device(x) for x in one), first=_ints([far - 1, 0]))
+        assert f.cache.status() == ckv.BAD_LENGTH
+        assert all(torch.equal(a, b) for a, b in zip(_raw(f.cache), before)), far
+    # five rows of which two lie below the limit
+    five = [bf16(f.rng.standard_normal((2, 5, 2, 128))) for _ in range(2)]
+    rows = [[x[b, :n].copy() for b, n in enumerate(f.lengths)] for x in f.rows]
+    for side in (0, 1):
+        rows[side][0][46:48], rows[side][1][25:30] = five[side][0, :2], five[side][1]
+    f.seqs.lengths.copy_(_ints([51, 30]))
+    f.cache.append(s, *(device(x) for x in five))
+    assert f.cache.status() == ckv.BAD_LENGTH
+    f.seqs.lengths.copy_(_ints(f.lengths))
+    _check_rows(f, rows)
+
+
+def test_rows_read_behind_the_largest_length_are_left_alone():
+    f = Filled([48, 30], 1, 16, True, seed=6)
+    s = f.cache.sequences(f.seqs.table, f.seqs.lengths, 48)
+    f.seqs.lengths.copy_(_ints([51, 30]))
+    out = tuple(torch.full((2, 5, 1, 128), 3.0, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    f.cache.read(s, 5, out=out)
+    assert f.cache.status() == ckv.BAD_LENGTH
+    for side in (0, 1):
+        got = out[side].double().cpu().numpy()
+        want = (f.k, f.v)[side]
+        assert np.array_equal(got[0, :2, 0], want[0][0][46:48]) and (got[0, 2:] == 3.0).all()
+        assert np.array_equal(got[1, :, 0], want[1][0][25:30])

@@ -27,3 +27,19 @@ def test_rows_go_to_the_positions_that_the_header_names(tmp_path):
               }
   const ckv::RowSpan s = ckv::row_span(100, 10, false, 0, true, 0, 3, 3);
   if (s.first != 97 || s.count != 3 || s.bad) return std::printf("%d %d\n", s.first, s.count), 1;""")
+
+
+def test_rows_behind_the_largest_length_are_left_out(tmp_path):
+    """Of a sequence of any length, whatever the array holds, the rows below the limit keep their positions."""
+    _run(tmp_path, r"""
+  for (int limit : {0, 1, 48, 1 << 30})
+    for (int length : {INT_MIN, -1, 0, 1, 47, 48, 49, 60, 1 << 30, (1 << 30) + 1, INT_MAX})
+      for (int most : {1, 5, 64, 1 << 30})
+        for (int has = 0; has < 2; ++has)
+          for (int first : {INT_MIN, -1, 0, 1, 40, 47, 48, 49, 1 << 30, INT_MAX}) {
+            const ckv::RowSpan all = ckv::row_span(length, most, has, first, false, 0, 0, 0), s = ckv::rows_below(all, limit);
+            const long long stop = (long long)all.first + all.count, end = stop < limit ? stop : limit;
+            const long long want = end > all.first ? end - all.first : 0;
+            if (s.bad != all.bad || s.count != want || s.first < 0 || (long long)s.first + s.count > limit || (want && s.first != all.first))
+              return std::printf("limit %d length %d rows %d first %d: %d, %d\n", limit, length, most, has ? first : -1, s.first, s.count), 1;
+          }""")
