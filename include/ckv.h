@@ -435,8 +435,9 @@ typedef struct {
   int32_t n_q_heads;
 } ckv_query;
 
-/* Writes rows into their pages and brings the pages' bounds up to date (those of a page whose first slot is written start anew; writing a
- * position again leaves bounds that still hold, if wider than need be).  No two rows of a call may go to the same place: sequences of one call
+/* Writes rows into their pages and brings the pages' bounds up to date: those of a page whose first slot is written are taken anew, from its rows up to lengths[b], written now
+ * or as they lie there; others are widened by the rows written.  So bounds hold whatever is written again, if wider than need be.  (A prompt written in parts needs lengths[b] = the part's
+ * end in each call: a row that is not there yet, but counts as the sequence's, widens its page's bounds by what the memory held.)  No two rows of a call may go to the same place: sequences of one call
  * must not share pages that it writes.  The rows of one sequence may reach 65535 pages in a call (CKV_EINVAL otherwise). */
 int ckv_paged_append(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_rows* rows, void* stream);
 

@@ -158,7 +158,7 @@ __global__ __launch_bounds__(NT) void paged_append_kernel(Paged p, Rows r) {
   const int u = blockIdx.x, b = u / p.hkv, h = u - b * p.hkv;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, piece = lane & 15, group = tid >> 4;
   int bad = 0;
-  p.length(b, bad);
+  const int length = p.length(b, bad);
   int64_t base;
   const RowSpan span = r.span(b, p.lengths[b], p.max_length, base);
   if (span.bad) bad |= PAGED_BAD_LENGTH;
@@ -175,6 +175,12 @@ __global__ __launch_bounds__(NT) void paged_append_kernel(Paged p, Rows r) {
   float lo[8], hi[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) lo[i] = INFINITY, hi[i] = -INFINITY;
+  auto widen = [&](u32x4 k) {
+    float x[8];
+    unpack8(k, x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) lo[i] = fminf(lo[i], x[i]), hi[i] = fmaxf(hi[i], x[i]);
+  };
   for (int row = begin + group; row < end; row += NT / 16) {
     const int64_t from = base + (int64_t)(row - span.first) * r.row_stride + h * r.head_stride + 16 * piece;
     const int slot = row & (p.page_size() - 1);
@@ -193,14 +199,23 @@ __global__ __launch_bounds__(NT) void paged_append_kernel(Paged p, Rows r) {
       *reinterpret_cast<u32x4*>(p.k + to) = k;
       *reinterpret_cast<u32x4*>(p.v + to) = v;
     }
-    if (p.bounds) {
-      float x[8];
-      unpack8(k, x);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) lo[i] = fminf(lo[i], x[i]), hi[i] = fmaxf(hi[i], x[i]);
-    }
+    if (p.bounds) widen(k);
   }
   if (!p.bounds) return;
+  const bool anew = (begin & (p.page_size() - 1)) == 0;
+  if (anew) {                                              // the page's rows behind those written, if the sequence has any
+    const int stop = min(length, (col + 1) << p.shift);
+    for (int row = end + group; row < stop; row += NT / 16) {
+      const int slot = row & (p.page_size() - 1);
+      const uint8_t* from = p.k + at + (int64_t)slot * p.slot_stride;
+      if constexpr (E4M3) {
+        const uint32_t e = p.scales[page * p.scale_page_stride + h * p.scale_head_stride + 2 * slot];
+        widen(values8(load8(from + 8 * piece), __uint_as_float(e << 23)));
+      } else {
+        widen(load16(from + 16 * piece));
+      }
+    }
+  }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     lo[i] = rows_combine(lo[i], [](float x, float y) { return fminf(x, y); });
@@ -219,7 +234,7 @@ __global__ __launch_bounds__(NT) void paged_append_kernel(Paged p, Rows r) {
     float x = s[0][d];
 #pragma unroll
     for (int w = 1; w < NT / 64; ++w) x = side ? fmaxf(x, s[w][d]) : fminf(x, s[w][d]);
-    if (begin & (p.page_size() - 1)) {                     // rows that were there before
+    if (!anew) {                                           // rows that were there before
       const float old = __uint_as_float((uint32_t)*to << 16);
       x = side ? fmaxf(x, old) : fminf(x, old);
     }

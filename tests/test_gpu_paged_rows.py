@@ -1,9 +1,10 @@
-"""Where the rows of a call go in a cache in pages: packed rows without their positions, lengths beyond the most that the
-call was told."""
+"""Where the rows of a call go in a cache in pages, and what a page's extremes cover: packed rows without their positions, lengths beyond the most that the
+call was told, rows written again."""
 import numpy as np
 import pytest
 import torch
 
+from oracle import paged as ref
 from tests.paged import DEV, Filled, bf16, device
 from paper_2601_16986_amd import ckv
 
@@ -26,6 +27,16 @@ def _check_rows(f, rows):
         for side, got in enumerate((k, v)):
             for h in range(f.hkv):
                 assert np.array_equal(got[0, :n, h].double().cpu().numpy(), f.held(rows[side][b][:n, h])), f"sequence {b} head {h}"
+
+
+def _check_bounds(f, rows):
+    bounds = f.cache.bounds.double().cpu().numpy()
+    for b, n in enumerate(f.lengths):
+        for c in range(-(-n // f.ps)):
+            for h in range(f.hkv):
+                lo, hi = ref.extremes(f.held(rows[0][b][c * f.ps:min(n, (c + 1) * f.ps), h]))
+                got = bounds[f.table[b, c], h]
+                assert np.array_equal(got[0], lo) and np.array_equal(got[1], hi), f"sequence {b} page {c} head {h}"
 
 
 # ------------------------------------------------------------------ packed rows without `first`
@@ -108,3 +119,59 @@ def test_rows_read_behind_the_largest_length_are_left_alone():
         want = (f.k, f.v)[side]
         assert np.array_equal(got[0, :2, 0], want[0][0][46:48]) and (got[0, 2:] == 3.0).all()
         assert np.array_equal(got[1, :, 0], want[1][0][25:30])
+
+
+# ------------------------------------------------------------------ rows written again
+@pytest.mark.parametrize("e4m3", [True, False])
+@pytest.mark.parametrize("ps,layout", [(16, "plain"), (64, "layers"), (256, "slots_first")])
+def test_a_page_s_first_rows_written_again(e4m3, ps, layout):
+    """A page's extremes cover its later rows too, however few of them the call writes, in the middle of a sequence and at its end."""
+    lengths = [3 * ps + ps // 2 + 1, ps, 2 * ps - 3]
+    f = Filled(lengths, 2, ps, e4m3, layout, seed=ps)
+    rows = [[x[b, :n].copy() for b, n in enumerate(lengths)] for x in f.rows]
+    for count, first in ((1, [0, 0, ps]), (1, [3 * ps, 0, 0]), (ps // 2, [2 * ps, 0, ps]), (ps + 1, [ps, 0, 0])):
+        new = [bf16(f.rng.standard_normal((3, count, 2, 128))) for _ in range(2)]
+        for side in (0, 1):
+            for b in range(3):
+                stop = min(lengths[b], first[b] + count)
+                rows[side][b][first[b]:stop] = new[side][b, :stop - first[b]]
+        f.cache.append(f.seqs, *(device(x) for x in new), first=_ints(first))
+        _check_rows(f, rows)
+        bounds = f.cache.bounds.double().cpu().numpy()
+        for b, n in enumerate(lengths):
+            for c in range(-(-n // ps)):
+                for h in range(2):
+                    lo, hi = ref.extremes(f.held(rows[0][b][c * ps:min(n, (c + 1) * ps), h]))
+                    got = bounds[f.table[b, c], h]
+                    assert (got[0] <= lo).all() and (got[1] >= hi).all(), f"{count} rows: sequence {b} page {c} head {h}"
+                    if first[b] == c * ps:              # written from its first slot on
+                        assert np.array_equal(got[0], lo) and np.array_equal(got[1], hi)
+    assert f.cache.status() == 0
+
+
+def test_a_page_with_a_rewritten_first_row_is_still_picked():
+    """The page that holds the one key along the query, behind a first row that is written again."""
+    f = Filled([16 * 12], 1, 16, True, seed=8, spread=0.1)
+    q = np.ones((1, 1, 128))
+    k = f.rows[0].copy()
+    k[0, 16 * 5 + 9] = 8.0
+    f.cache.append(f.seqs, device(k), device(f.rows[1]))
+    assert f.cache.select(f.seqs, device(q), 3).tolist() == [[[0, 5, 11]]]
+    f.cache.append(f.seqs, device(k[:, 80]), device(f.rows[1][:, 80]), first=_ints([80]))
+    assert f.cache.select(f.seqs, device(q), 3).tolist() == [[[0, 5, 11]]]
+
+
+@pytest.mark.parametrize("order", [[0, 1, 2], [2, 1, 0]])
+def test_a_prompt_in_parts_of_any_order(order):
+    """Parts that end inside pages: in ascending order, each with its end as length, extremes are exact; in any order they hold."""
+    f, ends = Filled([150], 2, 64, True, seed=9), [0, 40, 90, 150]
+    rows = [[x[0, :150]] for x in f.rows]
+    for x in (f.cache.k, f.cache.v):
+        x.view(torch.uint8).fill_(0x7F)
+    f.cache.bounds.fill_(float("nan"))
+    for i in order:
+        if order[0] == 0:
+            f.seqs.lengths.fill_(ends[i + 1])
+        f.cache.append(f.seqs, *(device(x[:, ends[i]:ends[i + 1]]) for x in f.rows), first=_ints([ends[i]]))
+    _check_rows(f, rows)
+    _check_bounds(f, rows)
