@@ -382,9 +382,9 @@ enum { CKV_PAGED_BAD_PAGE = 1,    /* a table entry that a sequence needs is not 
  *     to even; no number and infinities become the format's NaN); code * 2^E is
  *     a bf16 number (infinite where magnitudes from 3.3e38 on round up).  Caches that a caller fills need E in that range.
  *   bounds: dev bf16 [n_pages][n_kv_heads][2][128], or NULL: least and largest key
- *     value of each dimension over the page's rows (NaN left out), kept by
- *     ckv_paged_append and read by ckv_paged_select; strides in elements,
- *     multiples of 8, 16-byte aligned.
+ *     value of each dimension over the page's rows (NaN left out; +inf and -inf where
+ *     nothing is left, otherwise least <= largest), kept by ckv_paged_append and
+ *     read by ckv_paged_select; strides in elements, multiples of 8, 16-byte aligned.
  * page_size: 16, 32, 64, 128 or 256.  head_dim: 128. */
 typedef struct {
   int32_t n_pages, page_size, n_kv_heads, head_dim, dtype;

@@ -36,7 +36,8 @@ __device__ __forceinline__ float rows_combine(float v, Op op) {
   return op(__uint_as_float(h[0]), __uint_as_float(h[1]));
 }
 
-// Maxima that are NaN if an operand is.
+// Maxima and minima that are NaN if an operand is.
+__device__ __forceinline__ float min2(float a, float b) { return __builtin_elementwise_minimum(a, b); }
 __device__ __forceinline__ float max2(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 __device__ __forceinline__ float max3(float a, float b, float c) { return max2(max2(a, b), c); }
 

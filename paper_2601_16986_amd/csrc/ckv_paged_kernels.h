@@ -780,14 +780,17 @@ __device__ __forceinline__ void score_pages(const Paged& p, int b, int h, int he
 #pragma unroll
     for (int i = 0; i < 8; ++i) s = fma((double)hi[i], q.up[i], fma((double)lo[i], q.down[i], s));
     s = row_sum(s);
-    if (__any(s != s)) {                  // infinite extremes: where no query has a part of that sign the product is nothing
-      s = 0.0;
+    // Extremes that are infinite, or no numbers: where no query has a part of that sign the product is nothing, and a dimension without any number in the page has the larger
+    // one, +inf, as least.  (Least and largest put in order for all pages alike: 512 units of 293 pages 14.5 -> 15.5 us.)
+    if (__any(!(fabs(s) < INFINITY))) {
+      double t = 0.0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        if (q.up[i] != 0.0) s += hi[i] * q.up[i];
-        if (q.down[i] != 0.0) s += lo[i] * q.down[i];
+        if (q.up[i] != 0.0) t += max2(lo[i], hi[i]) * q.up[i];
+        if (q.down[i] != 0.0) t += min2(lo[i], hi[i]) * q.down[i];
       }
-      s = row_sum(s);
+      t = row_sum(t);
+      if (!(fabs(s) < INFINITY)) s = t;                  // (the wavefront's other pages keep theirs)
     }
     if (piece == 0 && first + n * step < held) put(first + n * step, page[n] < 0 ? -INFINITY : (float)s);
   }
