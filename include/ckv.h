@@ -445,7 +445,7 @@ int ckv_paged_append(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_row
 int ckv_paged_read(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_rows* rows, void* stream);
 
 /* Bytes of workspace that ckv_paged_attend needs (n_picked pages per KV head, 0: all entries), or ckv_paged_select (n_picked = -1), for these
- * sizes on the current device; it depends on max_length and the sizes alone.  256 if none is needed, 0 if the sizes are refused. */
+ * sizes on the current device; it depends on max_length and the sizes alone.  256 if none is needed, 0 if the sizes are refused (ckv_last_error says why). */
 size_t ckv_paged_workspace_bytes(const ckv_pages* pages, const ckv_seqs* seqs, int32_t n_q_heads, int32_t n_picked);
 
 /* Attention of one new token per sequence (whose own row has been appended): out[b][g] = softmax(softmax_scale q K^T) V over the sequence's

@@ -114,10 +114,15 @@ Rows rows_of(const ckv_rows* r) {
   return Rows{(uint8_t*)r->k, (uint8_t*)r->v, r->first, r->starts, r->seq_stride * 2, r->row_stride * 2, r->head_stride * 2, r->rows, r->total};
 }
 
+int check_heads(const ckv_pages* p, int n_q_heads) {
+  if (n_q_heads < p->n_kv_heads || n_q_heads % p->n_kv_heads != 0) return fail(CKV_EINVAL, "n_q_heads must be a multiple of n_kv_heads");
+  if (n_q_heads / p->n_kv_heads > kPagedGroup) return fail(CKV_EINVAL, "at most 16 query heads per KV head");
+  return CKV_OK;
+}
+
 int check_query(const ckv_pages* p, const ckv_query* q) {
   if (!q || !q->q || !aligned(q->q, 16)) return fail(CKV_EINVAL, "q must be a 16-byte aligned device address");
-  if (q->n_q_heads < p->n_kv_heads || q->n_q_heads % p->n_kv_heads != 0) return fail(CKV_EINVAL, "n_q_heads must be a multiple of n_kv_heads");
-  if (q->n_q_heads / p->n_kv_heads > kPagedGroup) return fail(CKV_EINVAL, "at most 16 query heads per KV head");
+  if (int rc = check_heads(p, q->n_q_heads)) return rc;
   if (!stride_ok(q->seq_stride, kDim, 8) || !stride_ok(q->head_stride, kDim, 8)) return fail(CKV_EINVAL, "strides of q must be at least 128 elements and multiples of 8");
   return CKV_OK;
 }
@@ -144,8 +149,10 @@ struct Split {
 };
 // Entries of a unit at most.
 long long unit_entries(const ckv_pages* p, const ckv_seqs* s, int n_picked) { return n_picked > 0 ? (long long)n_picked * p->page_size : s->max_length; }
-bool too_many(const ckv_pages* p, const ckv_seqs* s, int n_picked) {
-  return (long long)s->batch * p->n_kv_heads * unit_blocks((int)unit_entries(p, s, n_picked)) > (1ll << 30);
+int check_entries(const ckv_pages* p, const ckv_seqs* s, int n_picked) {
+  if ((long long)n_picked * p->page_size > kMaxLength) return fail(CKV_EINVAL, "too many pages picked");
+  if ((long long)s->batch * p->n_kv_heads * unit_blocks((int)unit_entries(p, s, n_picked)) > (1ll << 30)) return fail(CKV_EINVAL, "too many entries in all (2^35)");
+  return CKV_OK;
 }
 Split split_of(const ckv_pages* p, const ckv_seqs* s, int n_q_heads, int n_picked, int n_cu) {
   const long long units = (long long)s->batch * p->n_kv_heads;
@@ -207,9 +214,13 @@ int ckv_paged_read(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_rows*
 
 size_t ckv_paged_workspace_bytes(const ckv_pages* pages, const ckv_seqs* seqs, int32_t n_q_heads, int32_t n_picked) {
   if (check(pages, seqs) != CKV_OK) return 0;
-  if (n_q_heads < pages->n_kv_heads || n_q_heads % pages->n_kv_heads != 0 || n_q_heads / pages->n_kv_heads > kPagedGroup) return 0;
+  if (check_heads(pages, n_q_heads) != CKV_OK) return 0;
   if (n_picked == -1) return std::max<size_t>(256, score_bytes(pages, seqs, compute_units()));
-  if (n_picked < 0 || (long long)n_picked * pages->page_size > kMaxLength || too_many(pages, seqs, n_picked)) return 0;
+  if (n_picked < 0) {
+    fail(CKV_EINVAL, "n_picked must be -1 (a selection), 0 (all entries) or a number of pages");
+    return 0;
+  }
+  if (check_entries(pages, seqs, n_picked) != CKV_OK) return 0;
   return std::max<size_t>(256, split_of(pages, seqs, n_q_heads, n_picked, compute_units()).bytes());
 }
 
@@ -221,8 +232,7 @@ int ckv_paged_attend(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_que
   if (out_dtype != CKV_F32 && out_dtype != CKV_BF16) return fail(CKV_EINVAL, "out_dtype must be CKV_F32 or CKV_BF16");
   if (!(softmax_scale > 0.0f) || !std::isfinite(softmax_scale)) return fail(CKV_EINVAL, "softmax_scale must be positive");
   if (picked ? n_picked < 1 : n_picked != 0) return fail(CKV_EINVAL, "n_picked must be positive with a list of pages and 0 without");
-  if ((long long)n_picked * pages->page_size > kMaxLength) return fail(CKV_EINVAL, "too many pages picked");
-  if (too_many(pages, seqs, n_picked)) return fail(CKV_EINVAL, "too many entries in all (2^35)");
+  if (int rc = check_entries(pages, seqs, n_picked)) return rc;
   const int G = query->n_q_heads / pages->n_kv_heads;
   const Split s = split_of(pages, seqs, query->n_q_heads, n_picked, compute_units());
   if (s.bytes() > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < s.bytes())) return fail(CKV_EWORKSPACE, "workspace too small or misaligned");

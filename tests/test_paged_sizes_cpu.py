@@ -1,6 +1,11 @@
 """The cache in pages without a GPU: which positions rows of a call go to, how an attention is cut, and what refusals say.  The
 index arithmetic is that of the kernels, compiled on its own."""
-from tests.test_paged_cpu import _run
+import ctypes as C
+
+import pytest
+
+from paper_2601_16986_amd import ckv
+from tests.test_paged_cpu import _run, good  # noqa: F401
 
 
 # ------------------------------------------------------------------ rows
@@ -43,3 +48,18 @@ def test_rows_behind_the_largest_length_are_left_out(tmp_path):
             if (s.bad != all.bad || s.count != want || s.first < 0 || (long long)s.first + s.count > limit || (want && s.first != all.first))
               return std::printf("limit %d length %d rows %d first %d: %d, %d\n", limit, length, most, has ? first : -1, s.first, s.count), 1;
           }""")
+
+
+# ------------------------------------------------------------------ refusals
+@pytest.mark.parametrize("heads,picked,change,said", [
+    (7, 0, {}, b"multiple of n_kv_heads"), (0, 0, {}, b"multiple of n_kv_heads"), (34, -1, {}, b"16 query heads"), (8, -2, {}, b"n_picked"), (8, 1 << 27, {}, b"pages picked"),
+    (8, 0, dict(batch=1 << 22, columns=1 << 20, table_stride=1 << 20, max_length=1 << 24), b"too many entries")])
+def test_a_workspace_s_refusal_says_what_is_wrong(good, heads, picked, change, said):  # noqa: F811
+    """Not what another call was refused for before, nor nothing."""
+    lib = ckv.load()
+    pages, seqs = good[:2]
+    for k, v in change.items():
+        setattr(seqs, k, v)
+    assert lib.ckv_paged_append(None, None, None, None) == ckv.EINVAL and b"NULL" in lib.ckv_last_error(None)
+    assert lib.ckv_paged_workspace_bytes(C.addressof(pages), C.addressof(seqs), heads, picked) == 0
+    assert said in lib.ckv_last_error(None)
