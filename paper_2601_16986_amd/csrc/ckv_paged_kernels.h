@@ -355,12 +355,10 @@ __device__ __forceinline__ bool find_piece(const Paged& p, const Attend& c, int 
     }
     int share = attend_share(wave_sum_i32(blocks) * p.hkv, c.workers);
     if (per_lane == 1) {
-      // Units that end inside a share make more pieces than there are shares. Where units are few, larger pieces make up for it, so that no compute unit has more than
-      // its two (16 sequences x 8 heads of up to 9350 entries, bf16, 45.2 -> 41.5 us); of many units pieces would become too uneven (64 x 8 76.6 -> 92.5).
-      for (int i = 0; i < 2 && 4 * p.batch * p.hkv <= c.workers; ++i) {
+      for (int i = 0; i < 2 && enlarges_share(p.batch, p.hkv, c.workers); ++i) {
         const int all = wave_sum_i32(unit_parts(blocks, share)) * p.hkv;
         if (all <= c.workers) break;
-        share = (int)((float)share * (float)all / (float)c.workers) + 1;
+        share = larger_share(share, all, c.workers);
       }
       pieces = unit_parts(blocks, share);
       const int size = pieces ? unit_parts(blocks, pieces) : 0;
@@ -394,9 +392,8 @@ __device__ __forceinline__ bool find_piece(const Paged& p, const Attend& c, int 
     r.part = index - before - r.h * r.parts;
   }
   r.index = index;
-  const int even = n / r.parts, more = n - even * r.parts;      // the first `more` parts have a block more
-  r.first = r.part * even + min(r.part, more);
-  r.last = r.first + even + (r.part < more);
+  r.first = part_begin(n, r.parts, r.part);
+  r.last = part_begin(n, r.parts, r.part + 1);
   return true;
 }
 

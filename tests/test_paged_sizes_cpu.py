@@ -50,6 +50,69 @@ def test_rows_behind_the_largest_length_are_left_out(tmp_path):
           }""")
 
 
+# ------------------------------------------------------------------ how an attention is cut
+def test_every_piece_has_a_workgroup_and_a_place(tmp_path):
+    """Batches of any size and any lengths, each sequence's and head's unit counted: as many workgroups as pieces, parts only where the host expects them, and a unit's parts are its blocks."""
+    _run(tmp_path, r"""
+  static int length[4096];
+  unsigned seed = 1;
+  auto random = [&](long long n) { seed = seed * 1664525u + 1013904223u; return (int)((seed >> 8) % (unsigned long long)n); };
+  long long enlarged = 0, cut = 0, many = 0;
+  for (int batch : {1, 2, 3, 7, 15, 16, 17, 40, 63, 64, 65, 100, 128, 129, 300, 1000, 4096})
+    for (int hkv : {1, 2, 3, 8, 16, 64})
+      for (int n_cu : {256, 64})
+        for (long long most = 0; most <= (1 << 24); most = most * 2 + 1 + random(40)) {
+          const long long units = (long long)batch * hkv;
+          if (units * ckv::unit_blocks((int)most) > (1 << 30)) break;
+          for (bool same : {false, true}) {
+            const ckv::AttendPlan p = ckv::attend_plan(units, (int)most, same, n_cu);
+            for (int kind = 0; kind < 6; ++kind) {
+              long long blocks = 0;
+              for (int b = 0; b < batch; ++b) {
+                length[b] = kind == 0 || same ? (int)most : kind == 1 ? 0 : kind == 2 ? random(most + 1) : kind == 3 ? (b ? random(most / 50 + 1) : (int)most)
+                          : kind == 4 ? (int)(most / (1 + b % 7)) : (b % 3 ? (int)most : 1);
+                blocks += ckv::unit_blocks(length[b]);
+              }
+              auto pieces = [&](int share) {
+                long long n = 0;
+                for (int b = 0; b < batch; ++b) n += ckv::unit_parts(ckv::unit_blocks(length[b]), share);
+                return n * hkv;
+              };
+              int share = p.share;
+              if (!share) {
+                share = ckv::attend_share((int)(blocks * hkv), p.workers);
+                for (int i = 0; i < 2 && ckv::enlarges_share(batch, hkv, p.workers); ++i) {
+                  const long long all = pieces(share);
+                  if (all <= p.workers) break;
+                  const int before = share;
+                  share = ckv::larger_share(share, (int)all, p.workers);
+                  if (share < before) return std::printf("smaller share\n"), 1;
+                  ++enlarged;
+                }
+                if (pieces(share) > p.pieces) return std::printf("%lld pieces, %lld workgroups: %d x %d of up to %lld\n", pieces(share), p.pieces, batch, hkv, most), 1;
+                many += batch > 64;
+              } else if (units * p.places != p.pieces) {
+                return std::printf("%lld workgroups of %lld\n", p.pieces, units * p.places), 1;
+              }
+              for (int b = 0; b < batch; ++b) {
+                const int n = ckv::unit_blocks(length[b]), parts = ckv::unit_parts(n, share);
+                if (parts < 1 || parts > n || (parts > 1 && !p.split) || (p.share && parts > p.places)) return std::printf("%d parts of %d blocks\n", parts, n), 1;
+                if (kind < 4 && b > 4) continue;
+                int at = 0;
+                for (int i = 0; i < parts && i < 300; ++i) {
+                  const int first = ckv::part_begin(n, parts, i), last = ckv::part_begin(n, parts, i + 1);
+                  if (first != at || last <= first || last - first > share || last - first < n / parts) return std::printf("part %d of %d: %d .. %d\n", i, parts, first, last), 1;
+                  at = last;
+                }
+                if (parts <= 300 && at != n) return std::printf("%d of %d blocks\n", at, n), 1;
+                cut += parts > 1;
+              }
+            }
+          }
+        }
+  if (!enlarged || !cut || !many) return std::printf("%lld %lld %lld\n", enlarged, cut, many), 1;""")
+
+
 # ------------------------------------------------------------------ refusals
 @pytest.mark.parametrize("heads,picked,change,said", [
     (7, 0, {}, b"multiple of n_kv_heads"), (0, 0, {}, b"multiple of n_kv_heads"), (34, -1, {}, b"16 query heads"), (8, -2, {}, b"n_picked"), (8, 1 << 27, {}, b"pages picked"),
