@@ -637,7 +637,8 @@ class PagedCache:
         self._call(self.lib.ckv_paged_append, self._ref, seqs._ref, C.addressof(r))
 
     def read(self, seqs, rows, *, first=None, starts=None, total=None, out=None):
-        """The same rows back, bf16: (k, v), new tensors (uninitialised behind a sequence's last row) or `out`."""
+        """The same rows back, bf16: (k, v), new tensors (uninitialised behind a sequence's last row) or `out`, two alike tensors of any order of dimensions: over transposed
+        views of [batch][n_kv_heads][rows][128] they come as CrystalKV.load_prompt takes them."""
         if out is None:
             if starts is not None and total is None:
                 raise CkvError(EINVAL, "packed rows need `total` or `out`")
