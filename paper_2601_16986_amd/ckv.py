@@ -476,11 +476,19 @@ class PagedSequences:
             raise CkvError(EINVAL, "table needs a sequence, a column and contiguous rows, lengths must be contiguous")
         cache._same_device(table, lengths)
         self.batch, self.columns = table.shape
-        self.max_length = int(max_length) if max_length is not None else self.columns * cache.page_size
+        self.max_length = _int32(max_length if max_length is not None else self.columns * cache.page_size, "max_length")
         self.table, self.lengths, self.device = table, lengths, cache.device
         self._struct = Seqs(table.data_ptr(), lengths.data_ptr(), _stride(table, 0, self.columns), self.batch, self.columns, self.max_length)
         self._ref = C.addressof(self._struct)
         self._workspace = {}
+
+
+def _int32(x, what):
+    """A number as a 32-bit field takes it (ctypes would keep its lowest bits)."""
+    x = int(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise CkvError(EINVAL, f"{what} of {x} does not fit 32 bits")
+    return x
 
 
 def _stride(x, dim, unit):
@@ -591,6 +599,7 @@ class PagedCache:
             at_starts = self._numbers(starts, (seqs.batch + 1,), "starts must be int32 [batch + 1], contiguous")
             if rows is None:
                 raise CkvError(EINVAL, "packed rows need `rows`, the most that one sequence has")
+            rows = _int32(rows, "rows")
             if len(shape) != 3 or shape[1] != hkv or shape[2] != d:
                 raise CkvError(EINVAL, f"rows of shape {tuple(shape)}, [total][{hkv}][{d}] expected")
             total, row_stride, head_stride = shape[0], stride[0], stride[1]
@@ -674,13 +683,14 @@ class PagedCache:
         """`keep` pages per sequence and KV head for q: the `first` first, the `last` last, the others by score; int32 [batch][n_kv_heads][keep], ascending,
         -1 behind the last."""
         q_shape, query = self._query(seqs, q)
-        shape = (seqs.batch, self.n_kv_heads, int(keep))
+        keep, first, last = _int32(keep, "keep"), _int32(first, "first"), _int32(last, "last")
+        shape = (seqs.batch, self.n_kv_heads, keep)
         if out is None:
             out = self._status.new_empty(shape)
         else:
             self._numbers(out, shape, "out must be a contiguous int32 tensor [batch][n_kv_heads][keep]")
         work, at, n = self._workspace(seqs, q_shape[1], -1)
-        self._call(self.lib.ckv_paged_select, self._ref, seqs._ref, C.addressof(query), int(keep), int(first), int(last), out.data_ptr(), at, n)
+        self._call(self.lib.ckv_paged_select, self._ref, seqs._ref, C.addressof(query), keep, first, last, out.data_ptr(), at, n)
         return out
 
     def status(self):

@@ -42,3 +42,17 @@ def test_the_readme_s_loop():
     for side, x in (("K", k), ("V", v)):
         assert np.array_equal(e[side][order], x[1, 1].float().cpu().numpy())
     assert c.status() == 0 and g.status() == 0
+
+
+def test_numbers_beyond_32_bits_are_refused():
+    """Their lowest bits are numbers that the calls would take."""
+    f = Filled([20], 2, 16, True)
+    q, one = device(f.queries(4)), torch.zeros((1, 2, 128), dtype=torch.bfloat16, device=DEV)
+    starts = torch.tensor([0, 1], dtype=torch.int32, device=DEV)
+    before = f.cache.k.view(torch.uint8).clone()
+    for bad in (lambda: f.cache.sequences(f.seqs.table, f.seqs.lengths, 2 ** 32 + 20), lambda: f.cache.append(f.seqs, one, one, rows=2 ** 32 + 1, starts=starts),
+                lambda: f.cache.read(f.seqs, 2 ** 32 + 1, starts=starts, total=1), lambda: f.cache.select(f.seqs, q, 2, first=2 ** 32, last=0), lambda: f.cache.select(f.seqs, q, 2, first=0, last=2 ** 32 + 1),
+                lambda: f.cache.sequences(f.seqs.table, f.seqs.lengths, -2 ** 32 + 20)):
+        with pytest.raises(ckv.CkvError):
+            bad()
+    assert torch.equal(before, f.cache.k.view(torch.uint8))
