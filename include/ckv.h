@@ -404,7 +404,8 @@ typedef struct {
  * not looked at.  Sequences may share pages that nobody writes.  lengths: dev
  * [batch], entries of each sequence, in all calls of a step those of the step's
  * new rows included.  max_length <= columns * page_size: the most that a length
- * may be; launches and workspace are sized by it. */
+ * may be; launches and workspace are sized by it.  batch * n_kv_heads < 2^24 (in
+ * a selection 2^23, and 2^22 where sequences may have more than 2048 pages). */
 typedef struct {
   const int32_t* table;
   const int32_t* lengths;

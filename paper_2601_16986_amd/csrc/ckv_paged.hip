@@ -39,6 +39,9 @@ bool stride_ok(int64_t s, int64_t least, int64_t of) { return s >= least && s % 
 
 int element(const ckv_pages* p) { return p->dtype == CKV_E4M3 ? 1 : 2; }
 
+// Whether a launch of so many workgroups has fewer than 2^32 threads, the most that one axis takes.
+bool launches(long long groups, int threads) { return groups * threads < (1ll << 32); }
+
 int check(const ckv_pages* p, const ckv_seqs* s) {
   if (!p || !s) return fail(CKV_EINVAL, "pages or sequences are NULL");
   if (p->dtype != CKV_BF16 && p->dtype != CKV_E4M3) return fail(CKV_EINVAL, "dtype must be CKV_BF16 or CKV_E4M3");
@@ -65,7 +68,7 @@ int check(const ckv_pages* p, const ckv_seqs* s) {
   if (s->batch < 1 || s->columns < 1 || s->table_stride < s->columns || s->table_stride >= kMaxStride) return fail(CKV_EINVAL, "the table needs a row per sequence and a column per page");
   if (s->max_length < 0 || s->max_length > kMaxLength || s->max_length > (long long)s->columns * p->page_size)
     return fail(CKV_EINVAL, "max_length must be in [0, columns * page_size], at most 2^30");
-  if ((long long)s->batch * p->n_kv_heads > (1 << 24)) return fail(CKV_EINVAL, "too many sequences times KV heads");
+  if (!launches((long long)s->batch * p->n_kv_heads, kThreads)) return fail(CKV_EINVAL, "too many sequences times KV heads (2^24)");
   return CKV_OK;
 }
 
@@ -235,6 +238,7 @@ int ckv_paged_attend(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_que
   if (int rc = check_entries(pages, seqs, n_picked)) return rc;
   const int G = query->n_q_heads / pages->n_kv_heads;
   const Split s = split_of(pages, seqs, query->n_q_heads, n_picked, compute_units());
+  if (!launches(s.plan.pieces, kThreads)) return fail(CKV_EINVAL, "too many sequences times KV heads for one attention (2^24)");
   if (s.bytes() > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < s.bytes())) return fail(CKV_EWORKSPACE, "workspace too small or misaligned");
   const Paged p = paged_of(pages, seqs);
   Attend c{};
@@ -290,6 +294,7 @@ int ckv_paged_select(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_que
   c.keep_last = keep_last;
   c.score_stride = columns;
   const unsigned units = (unsigned)(seqs->batch * pages->n_kv_heads);
+  if (!launches(units, columns > 4 * kPickThreads ? kWideThreads : kPickThreads)) return fail(CKV_EINVAL, "too many sequences times KV heads for one selection (2^23; 2^22 of more than 2048 pages)");
   const int n_cu = compute_units();
   const bool past = bounds_past_caches(units, columns);
   if (selects_whole((int)units, columns, n_cu)) {

@@ -126,3 +126,18 @@ def test_a_workspace_s_refusal_says_what_is_wrong(good, heads, picked, change, s
     assert lib.ckv_paged_append(None, None, None, None) == ckv.EINVAL and b"NULL" in lib.ckv_last_error(None)
     assert lib.ckv_paged_workspace_bytes(C.addressof(pages), C.addressof(seqs), heads, picked) == 0
     assert said in lib.ckv_last_error(None)
+
+
+def test_batches_beyond_what_a_launch_takes_are_refused(good):  # noqa: F811
+    """2^32 threads on an axis: refused by the host's checks, not by the launch."""
+    lib = ckv.load()
+    pages, seqs, rows, query = good
+    p, s, r, q = (C.addressof(x) for x in good)
+    select = lambda: lib.ckv_paged_select(p, s, q, 3, 1, 1, 4096, 4096, 1 << 62, None)  # noqa: E731
+    attend = lambda: lib.ckv_paged_attend(p, s, q, 0.1, None, 0, 4096, ckv.BF16, None, 4096, 1 << 62, None)  # noqa: E731
+    for batch, columns, calls in ((1 << 23, 4, (lambda: lib.ckv_paged_append(p, s, r, None), lambda: lib.ckv_paged_read(p, s, r, None), attend, select)),
+                                  ((1 << 23) - 1, 100, (attend, select)), (1 << 22, 4, (select,)), (1 << 21, 2049, (select,))):
+        seqs.batch, seqs.columns, seqs.table_stride, seqs.max_length = batch, columns, columns, 16 * columns
+        for call in calls:
+            assert call() == ckv.EINVAL, (batch, columns)
+            assert b"2^2" in lib.ckv_last_error(None)
