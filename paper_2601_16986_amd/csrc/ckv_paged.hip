@@ -233,7 +233,8 @@ int ckv_paged_attend(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_que
   if (int rc = check_query(pages, query)) return rc;
   if (!out || !aligned(out, 16)) return fail(CKV_EINVAL, "out must be a 16-byte aligned device address");
   if (out_dtype != CKV_F32 && out_dtype != CKV_BF16) return fail(CKV_EINVAL, "out_dtype must be CKV_F32 or CKV_BF16");
-  if (!(softmax_scale > 0.0f) || !std::isfinite(softmax_scale)) return fail(CKV_EINVAL, "softmax_scale must be positive");
+  const float scale_log2e = softmax_scale * 1.44269504088896340736f;
+  if (!(softmax_scale > 0.0f) || !std::isfinite(scale_log2e)) return fail(CKV_EINVAL, "softmax_scale must be positive and below 2.3e38");
   if (picked ? n_picked < 1 : n_picked != 0) return fail(CKV_EINVAL, "n_picked must be positive with a list of pages and 0 without");
   if (int rc = check_entries(pages, seqs, n_picked)) return rc;
   const int G = query->n_q_heads / pages->n_kv_heads;
@@ -252,7 +253,7 @@ int ckv_paged_attend(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_que
   c.lse = lse;
   c.partial = (float*)workspace;
   c.ml = (float*)((char*)workspace + s.partial);
-  c.scale_log2e = softmax_scale * 1.44269504088896340736f;
+  c.scale_log2e = scale_log2e;
   c.G = G;
   if (s.plan.split) c.parts = (int32_t*)((char*)workspace + s.partial + s.ml);
   c.share = s.plan.share;

@@ -141,3 +141,11 @@ def test_batches_beyond_what_a_launch_takes_are_refused(good):  # noqa: F811
         for call in calls:
             assert call() == ckv.EINVAL, (batch, columns)
             assert b"2^2" in lib.ckv_last_error(None)
+
+
+def test_scales_whose_product_with_a_logarithm_is_infinite_are_refused(good):  # noqa: F811
+    lib = ckv.load()
+    p, s, _, q = (C.addressof(x) for x in good)
+    for scale in (2.4e38, 3.4e38):
+        assert lib.ckv_paged_attend(p, s, q, scale, None, 0, 4096, ckv.BF16, None, 4096, 1 << 30, None) == ckv.EINVAL
+        assert b"softmax_scale" in lib.ckv_last_error(None)
