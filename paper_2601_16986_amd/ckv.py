@@ -683,7 +683,9 @@ class PagedCache:
         """`keep` pages per sequence and KV head for q: the `first` first, the `last` last, the others by score; int32 [batch][n_kv_heads][keep], ascending,
         -1 behind the last."""
         q_shape, query = self._query(seqs, q)
-        keep, first, last = _int32(keep, "keep"), _int32(first, "first"), _int32(last, "last")
+        keep, first, last = int(keep), int(first), int(last)
+        if (keep | first | last) >> 31:
+            raise CkvError(EINVAL, f"keep, first and last must be in [0, 2^31), not {keep}, {first}, {last}")
         shape = (seqs.batch, self.n_kv_heads, keep)
         if out is None:
             out = self._status.new_empty(shape)
