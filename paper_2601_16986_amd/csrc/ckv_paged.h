@@ -63,7 +63,9 @@ CKV_PLAN int attend_share(int blocks, int workers) {
 }
 
 // Units that end inside a share make more pieces than there are shares. Where units are few, larger pieces make up for it, so that no compute unit has more than
-// its two (16 sequences x 8 heads of up to 9350 entries, bf16, 45.2 -> 41.5 us); of many units pieces would become too uneven (64 x 8 76.6 -> 92.5).
+// its two; of many units pieces would become too uneven.  Sequences of 8 heads, lengths spread up to 9350 entries, us, as they are / larger: bf16, 64 units 36.7 / 33.3, 96 45.1 / 41.2,
+// 128 46.9 / 43.0, 192 59.9 / 55.3, 256 92.9 / 92.8, 320 108 / 114, 384 112 / 118, 512 139 / 157; 8 bits, 128 28.8 / 27.8, 192 35.8 / 34.9, 256 53.0 / 53.1, 384 61.8 / 68.2.  (Taken up to 128
+// units of 256 compute units, clear of where it turns.)
 CKV_PLAN bool enlarges_share(int batch, int hkv, int workers) { return batch <= 64 && 4 * batch * hkv <= workers; }
 CKV_PLAN int larger_share(int share, int pieces, int workers) { return (int)((float)share * (float)pieces / (float)workers) + 1; }
 // First block of one of a unit's parts (that of part `parts` is `blocks`): the first ones have a block more.

@@ -149,7 +149,7 @@ __device__ __forceinline__ u32x4 values8(u32x2 codes, float scale) {
 
 // One workgroup per (sequence, KV head) and page that new rows reach: it alone touches the page's rows and extremes, so that these need no atomics.  Sixteen
 // lanes take a row, 16 bytes of bf16 each, for key and value.  Where rows are many it is bound by memory: 322208 rows (165 MB in, 83 MB out) 57 us, 4.3 TB/s, where a plain copy
-// reaches 4.7; magnitudes and codes from packed bf16 instead of floats were worth a fifth where the rows were in the caches (72192 rows 19.3 -> 16.1 us).  A single
+// reaches 4.7, as bf16 (165 MB out) 77 us, 4.3 TB/s; magnitudes and codes from packed bf16 instead of floats were worth a fifth where the rows were in the caches (72192 rows 19.3 -> 16.1 us).  A single
 // row of each of 32 sequences, 8 heads, takes 4 us: four dependent trips to memory.  (Spans of 64 rows of smaller pages, all rows asked for at once, took
 // longer: 69 us, and 6 instead of 4 for a prompt of 777.)
 template <bool E4M3, int NT>
@@ -406,10 +406,10 @@ __device__ __forceinline__ bool find_piece(const Paged& p, const Attend& c, int 
 //           dimensions 8 j + dt), in the entry order in which K Q^T leaves the logits.
 // The weights are split into three bf16 terms, which hold the 24 bits of a float: the high ones in rows 0 .. 7 and the second ones in rows 8 .. 15 of one operand for up to
 // eight heads (the queries are there twice), the third in another; operands of their own for more heads (WIDE).  (Two terms, 16
-// bits, whatever the output's type: 0.5 us less of 190, and outputs that nearly cancel off by 2^-18 of their terms.)
+// bits: 1 us less of 190, and outputs that nearly cancel off by 2^-18 of their terms.)
 //
-// It is bound by memory: 64 sequences x 8 KV heads of 9350 entries in 8 bits, 1236 MB (1243 by the counters), 189 us, 6.5 TB/s of the 7.1 of a plain read, and the same
-// without any of the arithmetic, which keeps the vector units busy for a fifth of the time.  Eight wavefronts per compute unit are enough, and more, or blocks asked
+// It is bound by memory: 64 sequences x 8 KV heads of 9350 entries in 8 bits, 1236 MB (1240 by the counters), 190 us, 6.5 TB/s of the 7.1 of a plain read, and the same
+// without any of the arithmetic, which keeps the vector units busy for a quarter of the time; 16 heads per KV head instead of 4 take 3 % longer, float outputs no longer.  Eight wavefronts per compute unit are enough, and more, or blocks asked
 // for one ahead, only make the streams more: 12 .. 16 of them 202 .. 217 us, 8 KB instead of 4 KB in flight each 191.  A piece costs some 3 us beside its
 // entries (length, page, rows: three trips; joining four wavefronts), so pieces are as few as fill the chip: twice, four, eight times as many 202, 205, 208 us.
 template <bool E4M3, bool WIDE>
