@@ -442,6 +442,31 @@ typedef struct {
  * must not share pages that it writes.  The rows of one sequence may reach 65535 pages in a call (CKV_EINVAL otherwise). */
 int ckv_paged_append(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_rows* rows, void* stream);
 
+/* Heads of a call's rows: head g of row i of sequence b lies at b * seq_stride + i * row_stride + g * head_stride, or, where the rows are packed, at
+ * (starts[b] + i) * row_stride + g * head_stride, which rows and sequences ckv_rows says (dev bf16, strides in elements, multiples of 8, 16-byte aligned). */
+typedef struct {
+  void* q;
+  int64_t seq_stride, row_stride, head_stride;
+  int32_t n_q_heads;      /* G * n_kv_heads with G <= 16 */
+} ckv_heads;
+
+/* A rotation by positions: of the first 2 n_pairs dimensions pair j turns by the angle a = position * frequencies[j] (dev double [n_pairs], radians per
+ * position), (x, y) -> magnitude * (x cos a - y sin a, y cos a + x sin a); pair j is the dimensions j and j + n_pairs, or 2 j and 2 j + 1 where interleaved is 1.  The other
+ * dimensions stay as they are.  n_pairs: a multiple of 8, 8 .. 64.  Angles are held in 64 bits, sines, cosines and what turns in 32. */
+typedef struct {
+  const double* frequencies;
+  int32_t n_pairs, interleaved;
+  float magnitude;
+} ckv_rotation;
+
+/* ckv_paged_append of keys that have not been rotated yet, and their rows' queries with them: a key is rotated, then rounded once, to bf16 or to codes and their power of two
+ * (infinities and no numbers as there, what turns into one among them); values enter as they are; queries go to q_out rotated and rounded to bf16 (q_out may be q).  positions:
+ * dev int32, one for each row, at b * rows + i or, where they are packed, starts[b] + i (drafted tokens that share a place in the text); NULL: the rows'
+ * positions in their sequence.  q: NULL (and q_out then too) where there is nothing but keys to rotate.  Queries of rows that are left out (ckv_rows; CKV_PAGED_BAD_LENGTH) and
+ * behind a sequence's last are not touched; those of a page that is not there are rotated. */
+int ckv_paged_append_rotated(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_rows* rows, const ckv_rotation* rotation, const int32_t* positions,
+                             const ckv_heads* q, const ckv_heads* q_out, void* stream);
+
 /* Reads rows back as bf16 (exact: see ckv_pages), up to 2^21 - 32 of a sequence in a call. */
 int ckv_paged_read(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_rows* rows, void* stream);
 

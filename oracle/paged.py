@@ -1,5 +1,5 @@
 """Plain CPU definitions of the cache in pages (ckv_paged_* of include/ckv.h) in 64 bits: what rows become in 8 bits, a page's extremes,
-attention of one token, and the pages that scores pick.  numpy; test infrastructure only."""
+attention of one token and of several rows, the pages that scores pick, and positions' rotations.  numpy; test infrastructure only."""
 from __future__ import annotations
 
 import math
@@ -93,3 +93,23 @@ def pick(score, keep, first, last):
     rest = sorted((i for i in range(held) if first <= i < held - last), key=lambda i: (0 if np.isnan(score[i]) else 1, 0.0 if np.isnan(score[i]) else -float(score[i]), i))
     out[:] = sorted(forced + rest[:keep - len(forced)])
     return out
+
+
+def rotate(x, positions, frequencies, interleaved=False, magnitude=1.0):
+    """Rows x [..., rows, heads, 128] turned by their positions [..., rows]."""
+    x, n = np.asarray(x, np.float64), len(frequencies)
+    first, second = (slice(0, 2 * n, 2), slice(1, 2 * n, 2)) if interleaved else (slice(0, n), slice(n, 2 * n))
+    angle = (np.asarray(positions, np.float64)[..., None] * np.asarray(frequencies, np.float64))[..., None, :]
+    c, s = magnitude * np.cos(angle), magnitude * np.sin(angle)
+    y = x.copy()
+    y[..., first], y[..., second] = x[..., first] * c - x[..., second] * s, x[..., second] * c + x[..., first] * s
+    return y
+
+
+def pair_size(x, n, interleaved=False):
+    """|x| + |y| of the pair that each dimension is in (0 where it is in none), of which a rounded rotation is off by a share."""
+    a = np.abs(np.asarray(x, np.float64))
+    first, second = (slice(0, 2 * n, 2), slice(1, 2 * n, 2)) if interleaved else (slice(0, n), slice(n, 2 * n))
+    y = np.zeros_like(a)
+    y[..., first] = y[..., second] = a[..., first] + a[..., second]
+    return y

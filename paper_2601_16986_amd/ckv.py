@@ -30,7 +30,7 @@ EXPORTS = [
     "ckv_rebudget", "ckv_rebalance", "ckv_pool_slots", "ckv_probe", "ckv_probe_noalloc", "ckv_get_budgets", "ckv_get_lengths", "ckv_get_segments", "ckv_set_budgets", "ckv_get_time",
     "ckv_set_time", "ckv_status", "ckv_export_unit", "ckv_import_unit", "ckv_profile_enable",
     "ckv_profile_read", "ckv_set_path", "ckv_path_info", "ckv_join", "ckv_bandwidth_probe", "ckv_strerror", "ckv_last_error",
-    "ckv_paged_append", "ckv_paged_read", "ckv_paged_workspace_bytes", "ckv_paged_attend", "ckv_paged_select",
+    "ckv_paged_append", "ckv_paged_append_rotated", "ckv_paged_read", "ckv_paged_workspace_bytes", "ckv_paged_attend", "ckv_paged_select",
 ]
 
 
@@ -73,6 +73,14 @@ class Rows(C.Structure):
 
 class Query(C.Structure):
     _fields_ = [("q", C.c_void_p), ("seq_stride", C.c_int64), ("head_stride", C.c_int64), ("n_q_heads", C.c_int32)]
+
+
+class Heads(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("seq_stride", C.c_int64), ("row_stride", C.c_int64), ("head_stride", C.c_int64), ("n_q_heads", C.c_int32)]
+
+
+class RotationParams(C.Structure):
+    _fields_ = [("frequencies", C.c_void_p), ("n_pairs", C.c_int32), ("interleaved", C.c_int32), ("magnitude", C.c_float)]
 
 
 _lib = None
@@ -122,6 +130,7 @@ def load():
     lib.ckv_join.argtypes = [vp, vp]
     lib.ckv_bandwidth_probe.argtypes = [vp, vp, C.c_size_t, vp, vp]
     lib.ckv_paged_append.argtypes = [vp, vp, vp, vp]
+    lib.ckv_paged_append_rotated.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp]
     lib.ckv_paged_read.argtypes = [vp, vp, vp, vp]
     lib.ckv_paged_workspace_bytes.restype = C.c_size_t
     lib.ckv_paged_workspace_bytes.argtypes = [vp, vp, i32, i32]
@@ -483,6 +492,19 @@ class PagedSequences:
         self._workspace = {}
 
 
+class Rotation:
+    """How positions turn queries and keys: pair j of the first 2 n dimensions by position * frequencies[j] (float64 [n] on the device, radians, n a multiple of 8 up to 64),
+    times `magnitude`.  Pair j is the dimensions j and j + n, or 2 j and 2 j + 1 (interleaved)."""
+
+    def __init__(self, frequencies, *, interleaved=False, magnitude=1.0):
+        import torch
+        if frequencies.dtype != torch.float64 or frequencies.dim() != 1 or not frequencies.is_contiguous() or frequencies.device.type != "cuda":
+            raise CkvError(EINVAL, "frequencies must be contiguous float64 [n] on the device")
+        self.frequencies, self.device = frequencies, frequencies.device
+        self._struct = RotationParams(frequencies.data_ptr(), frequencies.shape[0], 1 if interleaved else 0, magnitude)
+        self._ref = C.addressof(self._struct)
+
+
 def _int32(x, what):
     """A number as a 32-bit field takes it (ctypes would keep its lowest bits)."""
     x = int(x)
@@ -630,6 +652,22 @@ class PagedCache:
             self._same_device(q, seqs)
         return shape, Query(q.data_ptr(), stride[0] if shape[0] > 1 else self.head_dim, stride[1] if shape[1] > 1 else self.head_dim, shape[1])
 
+    def _row_heads(self, seqs, q, packed, rows, total):
+        """ckv_heads of queries [batch][rows][heads][128] ([batch][heads][128]: a row each; [total][heads][128] where they are packed)."""
+        shape, stride, d = q.shape, q.stride(), self.head_dim
+        if q.dtype is not self._bf16 or len(shape) not in (3, 4) or stride[-1] != 1 or shape[-1] != d or q.device != self.device:
+            raise CkvError(EINVAL, f"q must be bf16 rows of {d} on {self.device}, contiguous each")
+        heads = shape[-2]
+        if packed:
+            if len(shape) != 3 or shape[0] != total:
+                raise CkvError(EINVAL, f"q of shape {tuple(shape)}, [{total}][heads][{d}] expected")
+            seq, row = 0, stride[0] if total > 1 else d
+        else:
+            if shape[0] != seqs.batch or (shape[1] if len(shape) == 4 else 1) != rows:
+                raise CkvError(EINVAL, f"q of shape {tuple(shape)}, [{seqs.batch}][{rows}][heads][{d}] expected")
+            seq, row = stride[0] if shape[0] > 1 else d, stride[1] if rows > 1 else d
+        return Heads(q.data_ptr(), seq, row, stride[-2] if heads > 1 else d, heads)
+
     # ------------------------------------------------------------------ calls
     def sequences(self, table, lengths, max_length=None):
         """What the other calls take: table int32 [batch][columns] of page numbers, lengths int32 [batch]; max_length bounds the lengths (by
@@ -644,6 +682,31 @@ class PagedCache:
         `starts` its own number, at most `rows`)."""
         r = self._rows(seqs, k, v, rows, first, starts)
         self._call(self.lib.ckv_paged_append, self._ref, seqs._ref, C.addressof(r))
+
+    def append_rotated(self, seqs, q, k, v, rotation, *, positions=None, rows=None, first=None, starts=None, out=None):
+        """append of keys that a Rotation turns on the way, and of their queries, q bf16 [batch][rows][n_q_heads][128] (or as k and v otherwise): the turned queries, new (uninitialised
+        behind a sequence's last row) or `out`, which may be q.  positions: int32 [batch][rows] ([batch] of single rows, [total] with `starts`), contiguous; by default the rows' positions
+        in their sequences.  q None: keys alone."""
+        r = self._rows(seqs, k, v, rows, first, starts)
+        if rotation.device != self.device:
+            raise CkvError(EINVAL, f"a rotation on {rotation.device} with a cache on {self.device}")
+        packed = starts is not None
+        at_positions = None
+        if positions is not None:
+            at_positions = self._numbers(positions, (r.total,) if packed else tuple(k.shape[:-2]), "positions must be int32, contiguous, one for each row")
+        queries = turned = None
+        if q is not None:
+            queries = self._row_heads(seqs, q, packed, r.rows, r.total)
+            if out is None:
+                out = self.torch.empty_like(q) if q.is_contiguous() else self._like.new_empty(q.shape)
+            elif out.shape != q.shape:
+                raise CkvError(EINVAL, "out must be of q's shape")
+            turned = queries if out is q else self._row_heads(seqs, out, packed, r.rows, r.total)
+        elif out is not None:
+            raise CkvError(EINVAL, "out without q")
+        self._call(self.lib.ckv_paged_append_rotated, self._ref, seqs._ref, C.addressof(r), rotation._ref, at_positions, C.addressof(queries) if queries else None,
+                   C.addressof(turned) if turned else None)
+        return out
 
     def read(self, seqs, rows, *, first=None, starts=None, total=None, out=None):
         """The same rows back, bf16: (k, v), new tensors (uninitialised behind a sequence's last row) or `out`, two alike tensors of any order of dimensions: over transposed
