@@ -483,6 +483,39 @@ size_t ckv_paged_workspace_bytes(const ckv_pages* pages, const ckv_seqs* seqs, i
 int ckv_paged_attend(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_query* query, float softmax_scale, const int32_t* picked,
                      int32_t n_picked, void* out, int32_t out_dtype, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Queries of several rows per sequence (the next part of a prompt, drafted tokens, or a new token each), whose own keys and values have been appended: which rows of which sequences
+ * they are is said as in ckv_rows, and head g of row i of sequence b lies as in ckv_heads. */
+typedef struct {
+  const void* q;
+  const int32_t* first;
+  const int32_t* starts;
+  int64_t seq_stride, row_stride, head_stride;
+  int32_t rows, total, n_q_heads;
+} ckv_row_queries;
+
+/* What a row at position p of its sequence sees: entries e <= p, with window > 0 only those with e > p - window or e < sinks (window = 0: all, and sinks = 0).
+ *   tree: dev uint8 [batch][rows][rows] with strides in elements (the last dimension contiguous; tree_seq_stride 0: one for all sequences), or NULL.  The call's rows
+ * are then drafted tokens: row i sees all entries before the call's first row, and of the call's rows those j with tree[b][i][j] != 0 (itself only if it is among them).  Its
+ * position, for the window, is the number of entries before the call's rows plus that of rows it sees, less one; window, if any, must be at least `rows`, so that
+ * it never parts a row from those it names.  rows <= 512. */
+typedef struct {
+  int32_t window, sinks;
+  const uint8_t* tree;
+  int64_t tree_seq_stride, tree_row_stride;
+} ckv_mask;
+
+/* Bytes of workspace that ckv_paged_attend_rows needs for these sizes on the current device (256 if none, 0 if they are refused: ckv_last_error says why). */
+size_t ckv_paged_rows_workspace_bytes(const ckv_pages* pages, const ckv_seqs* seqs, int32_t rows, int32_t n_q_heads, const ckv_mask* mask);
+
+/* Attention of several rows per sequence: out[row][g] = softmax(softmax_scale q K^T) V over the entries that the row sees, out dev out_dtype
+ * [batch][rows][n_q_heads][128], or [total][n_q_heads][128] where rows are packed; lse as in ckv_paged_attend, dev float [batch][rows][n_q_heads] or [total][n_q_heads], or NULL.
+ * Rows behind a sequence's last, and those of ckv_paged_append that are left out, are not touched.  A row that sees nothing, or only logits of -inf, gets
+ * zeros and -inf.  Logits, statistics and sums are held in float, weights in 16 bits for bf16 outputs and in 24 for float ones.  Entries that a row does not see do not change its outputs, whatever
+ * they hold; one that it sees and gives weight must be finite (NaN comes out otherwise, in those dimensions).  Table entries of pages that no row of the call sees are not looked at: pages that have left
+ * every window can be given to other sequences.  A sequence's rows times query heads per KV head: below 2^31.  workspace: 256-byte aligned, NULL where 256 are needed. */
+int ckv_paged_attend_rows(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_row_queries* queries, const ckv_mask* mask, float softmax_scale, void* out,
+                          int32_t out_dtype, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Picks `keep` pages of each sequence and KV head for a token: the keep_first first and keep_last last ones (attention sinks, the latest
  * entries), and of the others those with the highest scores, where a page's score is the sum over the KV head's query heads of the largest q.k
  * that its bounds allow, sum_d max(q_d least_d, q_d largest_d), added up in 64 bits and rounded once to float (a zero of q adds nothing, whatever the bounds; no number

@@ -75,6 +75,36 @@ def attend(q, k, v, scale):
     return (w[:, None] * v).sum(0) / w_sum, m + math.log(w_sum), (w[:, None] * np.abs(v)).sum(0) / w_sum, reach
 
 
+def sees(first, rows, window=0, sinks=0, tree=None):
+    """Which of the first + rows entries of a sequence each of its last `rows` rows sees, bool [rows][first + rows]."""
+    e, i = np.arange(first + rows)[None], np.arange(rows)[:, None]
+    if tree is None:
+        p = first + i
+        m = e <= p
+    else:
+        tree = np.asarray(tree, bool)[:rows, :rows]
+        p = first + tree.sum(1, keepdims=True) - 1
+        m = np.concatenate([np.ones((rows, first), bool), tree], 1)
+    return m & ((e > p - window) | ((e < sinks) & (e <= p) if tree is None else (e < sinks))) if window else m
+
+
+def attend_rows(q, k, v, mask, scale):
+    """Rows q [rows][128] over entries k, v [n][128] as far as mask [rows][n] says: outputs, lse, sums of |weight * value|, largest sum |q k| scale of each row."""
+    n = len(q)
+    if k.shape[0] == 0:
+        return np.zeros((n, D)), np.full(n, -np.inf), np.zeros((n, D)), np.zeros(n)
+    with np.errstate(invalid="ignore", divide="ignore"):
+        s = np.where(mask, (q @ np.where(mask.any(0)[:, None], k, 0.0).T) * scale, -np.inf)
+        m = s.max(1, keepdims=True)
+        w = np.exp(s - np.where(np.isinf(m), 0.0, m))
+        total = w.sum(1)
+        some = np.where(total > 0, total, 1.0)
+        clean = np.where(np.isfinite(v), v, 0.0)
+        out, mass = w @ clean / some[:, None], w @ np.abs(clean) / some[:, None]
+        reach = np.where(s > -np.inf, (np.abs(q) @ np.abs(np.where(np.isfinite(k), k, 0.0)).T) * scale, 0.0).max(1)
+        return out, np.where(total > 0, m[:, 0] + np.log(some), -np.inf), mass, reach
+
+
 def scores(q, lo, hi):
     """Scores of pages: q [G][128], lo, hi [pages][128].  A zero of a query adds nothing, whatever the extremes."""
     q = np.asarray(q, np.float64)

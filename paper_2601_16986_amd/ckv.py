@@ -30,7 +30,8 @@ EXPORTS = [
     "ckv_rebudget", "ckv_rebalance", "ckv_pool_slots", "ckv_probe", "ckv_probe_noalloc", "ckv_get_budgets", "ckv_get_lengths", "ckv_get_segments", "ckv_set_budgets", "ckv_get_time",
     "ckv_set_time", "ckv_status", "ckv_export_unit", "ckv_import_unit", "ckv_profile_enable",
     "ckv_profile_read", "ckv_set_path", "ckv_path_info", "ckv_join", "ckv_bandwidth_probe", "ckv_strerror", "ckv_last_error",
-    "ckv_paged_append", "ckv_paged_append_rotated", "ckv_paged_read", "ckv_paged_workspace_bytes", "ckv_paged_attend", "ckv_paged_select",
+    "ckv_paged_append", "ckv_paged_append_rotated", "ckv_paged_read", "ckv_paged_workspace_bytes", "ckv_paged_attend", "ckv_paged_rows_workspace_bytes", "ckv_paged_attend_rows",
+    "ckv_paged_select",
 ]
 
 
@@ -77,6 +78,16 @@ class Query(C.Structure):
 
 class Heads(C.Structure):
     _fields_ = [("q", C.c_void_p), ("seq_stride", C.c_int64), ("row_stride", C.c_int64), ("head_stride", C.c_int64), ("n_q_heads", C.c_int32)]
+
+
+class RowQueries(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("first", C.c_void_p), ("starts", C.c_void_p),
+                ("seq_stride", C.c_int64), ("row_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("rows", C.c_int32), ("total", C.c_int32), ("n_q_heads", C.c_int32)]
+
+
+class Mask(C.Structure):
+    _fields_ = [("window", C.c_int32), ("sinks", C.c_int32), ("tree", C.c_void_p), ("tree_seq_stride", C.c_int64), ("tree_row_stride", C.c_int64)]
 
 
 class RotationParams(C.Structure):
@@ -135,6 +146,9 @@ def load():
     lib.ckv_paged_workspace_bytes.restype = C.c_size_t
     lib.ckv_paged_workspace_bytes.argtypes = [vp, vp, i32, i32]
     lib.ckv_paged_attend.argtypes = [vp, vp, vp, C.c_float, vp, i32, vp, i32, vp, vp, C.c_size_t, vp]
+    lib.ckv_paged_rows_workspace_bytes.restype = C.c_size_t
+    lib.ckv_paged_rows_workspace_bytes.argtypes = [vp, vp, i32, i32, vp]
+    lib.ckv_paged_attend_rows.argtypes = [vp, vp, vp, vp, C.c_float, vp, i32, vp, vp, C.c_size_t, vp]
     lib.ckv_paged_select.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, C.c_size_t, vp]
     lib.ckv_strerror.restype = C.c_char_p
     lib.ckv_strerror.argtypes = [C.c_int]
@@ -591,14 +605,15 @@ class PagedCache:
         if rc != OK:
             raise CkvError(rc, self.lib.ckv_last_error(None).decode())
 
-    def _workspace(self, seqs, n_q_heads, n_picked):
-        """(tensor, address, bytes) of a workspace for a call of these sizes, from torch's allocator, which keeps calls on different streams, and in captured
+    def _workspace(self, seqs, n_q_heads, n_picked, at_mask=None):
+        """(tensor, address, bytes) of a workspace for a call of these sizes (n_picked: the rows and the mask's sizes where at_mask is one), from torch's allocator, which keeps calls on different streams, and in captured
         graphs, apart; none where none is needed."""
         key = (n_q_heads, n_picked, self._geometry)
         n = seqs._workspace.get(key)
         if n is None:
             with self.torch.cuda.device(self.device):
-                n = self.lib.ckv_paged_workspace_bytes(self._ref, seqs._ref, n_q_heads, n_picked)
+                n = self.lib.ckv_paged_workspace_bytes(self._ref, seqs._ref, n_q_heads, n_picked) if at_mask is None else \
+                    self.lib.ckv_paged_rows_workspace_bytes(self._ref, seqs._ref, n_picked[0], n_q_heads, at_mask)
             if n == 0:
                 raise CkvError(EINVAL, self.lib.ckv_last_error(None).decode())
             seqs._workspace[key] = n
@@ -740,6 +755,49 @@ class PagedCache:
         work, at, n = self._workspace(seqs, shape[1], n_picked)
         self._call(self.lib.ckv_paged_attend, self._ref, seqs._ref, C.addressof(query), self._scale if scale is None else scale, at_pages, n_picked, out.data_ptr(),
                    F32 if f32 else BF16, sums.data_ptr() if lse else None, at, n)
+        return out, sums
+
+    def attend_rows(self, seqs, q, *, window=0, sinks=0, tree=None, rows=None, first=None, starts=None, scale=None, f32=False, lse=False, out=None):
+        """Attention of several rows per sequence, whose own rows have been appended: q bf16 [batch][rows][n_q_heads][128] ([batch][n_q_heads][128]: one each), or with `starts` [total][n_q_heads][128]
+        and `rows` the most that one sequence has; they are the rows that append would take them for.  Each sees what comes before it and itself; with `window` only so many entries (itself
+        included) and the first `sinks`; with `tree`, bool [batch][rows][rows] or [rows][rows] for all, everything before the call's rows and those of them that its line names.
+        Returns (out, lse): of q's shape in bf16 or float (f32), lse float without the last dimension or None; uninitialised behind a sequence's last row."""
+        shape, packed = q.shape, starts is not None
+        at_first = self._numbers(first, (seqs.batch,), "first must be int32 [batch], contiguous") if first is not None else None
+        at_starts = None
+        if packed:
+            at_starts = self._numbers(starts, (seqs.batch + 1,), "starts must be int32 [batch + 1], contiguous")
+            if rows is None:
+                raise CkvError(EINVAL, "packed rows need `rows`, the most that one sequence has")
+            rows = _int32(rows, "rows")
+        else:
+            count = shape[1] if len(shape) == 4 else 1
+            if rows is not None and rows != count:
+                raise CkvError(EINVAL, f"q of shape {tuple(shape)} with {rows} rows")
+            rows = count
+        if seqs.device != self.device:
+            self._same_device(seqs)
+        total = shape[0] if packed else 0
+        h = self._row_heads(seqs, q, packed, rows, total)
+        mask = Mask(_int32(window, "window"), _int32(sinks, "sinks"), None, 0, 0)
+        if tree is not None:
+            t = self.torch
+            if tree.dtype not in (t.bool, t.uint8) or tree.shape not in ((seqs.batch, rows, rows), (rows, rows)) or (rows > 1 and tree.stride(-1) != 1):
+                raise CkvError(EINVAL, f"tree must be bool [{seqs.batch}][{rows}][{rows}] or [{rows}][{rows}] with contiguous lines")
+            self._same_device(tree)
+            mask.tree, mask.tree_row_stride = tree.data_ptr(), tree.stride(-2) if rows > 1 else 1
+            mask.tree_seq_stride = tree.stride(0) if tree.dim() == 3 and seqs.batch > 1 else 0
+        query = RowQueries(q.data_ptr(), at_first, at_starts, h.seq_stride, h.row_stride, h.head_stride, rows, total, h.n_q_heads)
+        dtype = self._f32 if f32 else self._bf16
+        if out is None:
+            out = self.torch.empty_like(q, dtype=dtype) if q.is_contiguous() else self._like.new_empty(shape, dtype=dtype)
+        elif out.dtype is not dtype or out.shape != shape or not out.is_contiguous() or out.device != self.device:
+            raise CkvError(EINVAL, f"out must be a contiguous {dtype} tensor of q's shape")
+        sums = self._like.new_empty(shape[:-1], dtype=self._f32) if lse else None
+        at_mask = C.addressof(mask)
+        work, at, n = self._workspace(seqs, h.n_q_heads, (rows, mask.window, mask.sinks, tree is not None), at_mask)
+        self._call(self.lib.ckv_paged_attend_rows, self._ref, seqs._ref, C.addressof(query), at_mask, self._scale if scale is None else scale, out.data_ptr(), F32 if f32 else BF16,
+                   sums.data_ptr() if lse else None, at, n)
         return out, sums
 
     def select(self, seqs, q, keep, *, first=1, last=1, out=None):

@@ -15,10 +15,10 @@ struct Turned {
   int32_t G, pairs, interleaved;
 };
 
-// Sine and cosine of the angle p * f, rounded to float.  A position times a frequency has more digits than a float keeps of a far angle (131072 rad to 2^-7), so it
+// Sine and cosine of the angle p * f, times the magnitude.  A position times a frequency has more digits than a float keeps of a far angle (131072 rad to 2^-7), so it
 // is 64 bits that count turns; what is left of them, an eighth at most to either side of the nearest quarter, goes into the Taylor series of both, in 64 bits
 // too (as fast as 32 here), up to terms of 2^-33.
-__device__ __forceinline__ void sine_cosine(int p, double f, float magnitude, float& sine, float& cosine) {
+__device__ __forceinline__ void sine_cosine(int p, double f, float magnitude, double& sine, double& cosine) {
   const double turns = (double)p * f * 0.15915494309189533577, quarters = rint(turns * 4.0);
   const double x = fma(quarters, -0.25, turns) * 6.28318530717958647693, y = x * x;
   double s = fma(y, fma(y, -1.0 / 39916800, 1.0 / 362880), -1.0 / 5040), c = fma(y, -1.0 / 3628800, 1.0 / 40320);
@@ -26,8 +26,23 @@ __device__ __forceinline__ void sine_cosine(int p, double f, float magnitude, fl
   c = fma(y, fma(y, fma(y, fma(y, c, -1.0 / 720), 1.0 / 24), -0.5), 1.0);
   const int quarter = (int)(quarters - 4.0 * floor(quarters * 0.25));         // 0 .. 3
   const double a = quarter & 1 ? c : s, b = quarter & 1 ? s : c;
-  sine = (float)((quarter & 2 ? -a : a) * magnitude);
-  cosine = (float)((quarter == 1 || quarter == 2 ? -b : b) * magnitude);
+  sine = (quarter & 2 ? -a : a) * magnitude;
+  cosine = (quarter == 1 || quarter == 2 ? -b : b) * magnitude;
+}
+
+// A value in 64 bits to 32 with the rest remembered in the lowest bit (towards zero, and odd where that is not exact), so that rounding it to fewer bits is one rounding.
+__device__ __forceinline__ float to_odd(double y) {
+  const float f = (float)y;
+  uint32_t b = __float_as_uint(f);
+  if (fabs((double)f) > fabs(y)) --b;
+  return fabsf(f) < INFINITY ? __uint_as_float((double)f != y ? b | 1u : b) : f;
+}
+
+__device__ __forceinline__ float of_lane(float v, int lane) { return __int_as_float(__builtin_amdgcn_ds_bpermute(lane << 2, __float_as_int(v))); }
+__device__ __forceinline__ double of_lane(double v, int lane) {
+  const long long x = __double_as_longlong(v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_ds_bpermute(lane << 2, (int)(uint32_t)x), hi = (uint32_t)__builtin_amdgcn_ds_bpermute(lane << 2, (int)(uint32_t)(x >> 32));
+  return __longlong_as_double((long long)((u64)hi << 32 | lo));
 }
 
 // Largest finite magnitude (its bits) of a row that 16 lanes hold, 8 floats each.
@@ -58,14 +73,33 @@ __device__ __forceinline__ u32x2 quantise8(const float (&x)[8], uint32_t& e) {
   return codes;
 }
 
-// Eight values of a row that sixteen lanes hold, turned: s and c for each of them, s negative where the value is a pair's first; `turn`: whether the lane's values are in
-// pairs at all, with whom it exchanges them at `partner` (none where pairs lie side by side).
-struct Turn {
-  float s[8], c[8];
-  int partner;
-  bool turn, exchange;
-  __device__ __forceinline__ void operator()(u32x4 x, float (&y)[8]) const {
-    float a[8], z[8];
+// How sixteen lanes turn a row, eight values each: with whom a lane exchanges them (nobody where pairs lie side by side), which lane worked out the first four pairs of its
+// eight (or four), whether its values are a pair's first ones, and whether they are in pairs at all.
+struct Pairing {
+  int partner, from;
+  bool exchange, first, turn;
+  __device__ __forceinline__ Pairing(int lane, int pairs, bool interleaved) {
+    const int piece = lane & 15, row = lane & 48, half = pairs >> 3;
+    exchange = !interleaved;
+    first = piece < half;
+    turn = piece < 2 * half;
+    const int other = first ? piece + half : turn ? piece - half : piece;
+    partner = row + other;
+    from = row + (interleaved ? piece : turn ? 2 * min(piece, other) : 0);
+  }
+  // of four pairs per lane the sine and cosine of its value k, a pair's first value with the sine's other sign
+  template <class T>
+  __device__ __forceinline__ void spread(const double (&sine)[4], const double (&cosine)[4], int k, T& s, T& c) const {
+    if (exchange) {
+      s = of_lane((T)sine[k & 3], from + (k >> 2));
+      c = of_lane((T)cosine[k & 3], from + (k >> 2));
+      if (first) s = -s;
+    } else {
+      s = (T)(k & 1 ? sine[k >> 1] : -sine[k >> 1]);
+      c = (T)cosine[k >> 1];
+    }
+  }
+  __device__ __forceinline__ void values(u32x4 x, float (&a)[8], float (&z)[8]) const {
     unpack8(x, a);
     if (exchange) {
       u32x4 other;
@@ -76,8 +110,26 @@ struct Turn {
 #pragma unroll
       for (int i = 0; i < 8; ++i) z[i] = a[i ^ 1];
     }
+  }
+  __device__ __forceinline__ u32x4 bf16(u32x4 x, const float (&s)[8], const float (&c)[8]) const {
+    float a[8], z[8], y[8];
+    values(x, a, z);
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = turn ? fmaf(a[i], c[i], z[i] * s[i]) : a[i];
+    return u32x4{bf16_pack(y[0], y[1]), bf16_pack(y[2], y[3]), bf16_pack(y[4], y[5]), bf16_pack(y[6], y[7])};
+  }
+  // Keys in 8 bits stay in 64 until they are rounded: a bf16 number is half way between two codes often enough (one in thirty-two), and slow pairs turn it by less than a
+  // float's last bit.
+  __device__ __forceinline__ u32x2 codes(u32x4 x, const double (&sine)[4], const double (&cosine)[4], uint32_t& e) const {
+    float a[8], z[8], y[8];
+    values(x, a, z);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      double s, c;
+      spread(sine, cosine, i, s, c);
+      y[i] = turn ? to_odd(fma((double)a[i], c, (double)z[i] * s)) : a[i];
+    }
+    return quantise8(y, e);
   }
 };
 
@@ -113,80 +165,64 @@ __global__ __launch_bounds__(kThreads) void paged_append_rotated_kernel(Paged p,
   double f[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) f[i] = 4 * piece + i < c.pairs ? c.frequencies[4 * piece + i] : 0.0;
-  Turn t;
-  const int half = c.pairs >> 3;                       // pieces that hold the pairs' first values
-  t.exchange = !c.interleaved;
-  t.turn = piece < 2 * half;
-  t.partner = (lane & 48) + (piece < half ? piece + half : t.turn ? piece - half : piece);
-  const int mine = (lane & 48) + (c.interleaved ? piece : 2 * (piece < half ? piece : t.turn ? piece - half : 0));      // the lane with the first four pairs of this one's
+  const Pairing t(lane, c.pairs, c.interleaved);
 
   int parts = 1;                                       // of a row's heads
   while (parts < kGroups && 2 * parts * (end - begin) <= kGroups) parts *= 2;
-  const int part = group & (parts - 1), heads = c.G + 1;        // the key and value, then the queries
+  const int part = group & (parts - 1), heads = c.G + 1, rows_each = kGroups / parts;       // the key and value, then the queries
   Extremes<E4M3, kThreads> extremes;
-  const int rows_each = kGroups / parts;
-  for (int row0 = begin; row0 < end; row0 += rows_each) {
-    const int row = min(row0 + group / parts, end - 1);
-    const bool there = row0 + group / parts < end;
+  for (int row = begin + group / parts; row < end; row += rows_each) {
     const int i = row - span.first, slot = row & (p.page_size() - 1), position = positions ? positions[i] : row;
-    float sine[4], cosine[4];
+    u32x4 x[kTurnAhead], v = {0u, 0u, 0u, 0u};
+    auto ask = [&](int first) {
+#pragma unroll
+      for (int n = 0; n < kTurnAhead; ++n) {
+        const int head = first + n * parts;
+        if (head > 0 && head < heads) x[n] = load16(q0 + i * c.q_row + (head - 1) * c.q_head);
+      }
+    };
+    if (part == 0) {
+      const int64_t from = base + (int64_t)i * r.row_stride + h * r.head_stride + 16 * piece;
+      x[0] = load16(r.k + from);
+      v = load16(r.v + from);
+    }
+    ask(part);
+    double sine[4], cosine[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) sine_cosine(position, f[k], c.magnitude, sine[k], cosine[k]);
-    if (c.interleaved) {
+    float fs[8], fc[8];
+    auto floats = [&]() {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        t.c[k] = cosine[k >> 1];
-        t.s[k] = k & 1 ? sine[k >> 1] : -sine[k >> 1];
+      for (int k = 0; k < 8; ++k) t.spread(sine, cosine, k, fs[k], fc[k]);
+    };
+    if constexpr (!E4M3) floats();
+    if (part == 0 && page >= 0) {
+      u32x4 k;
+      if constexpr (E4M3) {
+        uint32_t ek, ev;
+        const u32x2 ck = t.codes(x[0], sine, cosine, ek), cv = quantise8(v, ev);
+        const int64_t to = at + (int64_t)slot * p.slot_stride + 8 * piece;
+        *reinterpret_cast<u32x2*>(p.k + to) = ck;
+        *reinterpret_cast<u32x2*>(p.v + to) = cv;
+        if (piece == 0)
+          *reinterpret_cast<uint16_t*>(p.scales + page * p.scale_page_stride + h * p.scale_head_stride + 2 * slot) = (uint16_t)(ek | ev << 8);
+        k = values8(ck, __uint_as_float(ek << 23));
+      } else {
+        k = t.bf16(x[0], fs, fc);
+        const int64_t to = at + (int64_t)slot * p.slot_stride + 16 * piece;
+        *reinterpret_cast<u32x4*>(p.k + to) = k;
+        *reinterpret_cast<u32x4*>(p.v + to) = v;
       }
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        t.c[k] = __int_as_float(__builtin_amdgcn_ds_bpermute((mine + (k >> 2)) << 2, __float_as_int(cosine[k & 3])));
-        const float s = __int_as_float(__builtin_amdgcn_ds_bpermute((mine + (k >> 2)) << 2, __float_as_int(sine[k & 3])));
-        t.s[k] = piece < half ? -s : s;
-      }
+      if (p.bounds) extremes.widen(k);
     }
+    if constexpr (E4M3) floats();
     for (int first = part; first < heads; first += parts * kTurnAhead) {
-      u32x4 x[kTurnAhead], v = {0u, 0u, 0u, 0u};
+      if (first != part) ask(first);
 #pragma unroll
       for (int n = 0; n < kTurnAhead; ++n) {
         const int head = first + n * parts;
-        if (head == 0) {
-          const int64_t from = base + (int64_t)i * r.row_stride + h * r.head_stride + 16 * piece;
-          x[n] = load16(r.k + from);
-          v = load16(r.v + from);
-        } else if (head < heads) {
-          x[n] = load16(q0 + i * c.q_row + (head - 1) * c.q_head);
-        } else {
-          x[n] = u32x4{0u, 0u, 0u, 0u};
-        }
-      }
-#pragma unroll
-      for (int n = 0; n < kTurnAhead; ++n) {
-        const int head = first + n * parts;
-        float y[8];
-        t(x[n], y);
-        const u32x4 packed = {bf16_pack(y[0], y[1]), bf16_pack(y[2], y[3]), bf16_pack(y[4], y[5]), bf16_pack(y[6], y[7])};
-        if (head > 0) {
-          if (head < heads && there) *reinterpret_cast<u32x4*>(out0 + i * c.out_row + (head - 1) * c.out_head) = packed;
-        } else if (n == 0 && page >= 0 && there) {
-          u32x4 k = packed;
-          if constexpr (E4M3) {
-            uint32_t ek, ev;
-            const u32x2 ck = quantise8(y, ek), cv = quantise8(v, ev);
-            const int64_t to = at + (int64_t)slot * p.slot_stride + 8 * piece;
-            *reinterpret_cast<u32x2*>(p.k + to) = ck;
-            *reinterpret_cast<u32x2*>(p.v + to) = cv;
-            if (piece == 0)
-              *reinterpret_cast<uint16_t*>(p.scales + page * p.scale_page_stride + h * p.scale_head_stride + 2 * slot) = (uint16_t)(ek | ev << 8);
-            k = values8(ck, __uint_as_float(ek << 23));
-          } else {
-            const int64_t to = at + (int64_t)slot * p.slot_stride + 16 * piece;
-            *reinterpret_cast<u32x4*>(p.k + to) = k;
-            *reinterpret_cast<u32x4*>(p.v + to) = v;
-          }
-          if (p.bounds) extremes.widen(k);
-        }
+        if (head == 0 || head >= heads) continue;
+        *reinterpret_cast<u32x4*>(out0 + i * c.out_row + (head - 1) * c.out_head) = t.bf16(x[n], fs, fc);
       }
     }
   }
