@@ -6,12 +6,12 @@ namespace ckv {
 
 typedef unsigned long long u64_t;
 
-constexpr int kTile = 64;              // entries that a workgroup takes at once (of its two halves or four quarters where its wavefronts divide entries: see rows_tile)
 constexpr int kMaxDrafts = 512;        // rows of a sequence in a call with a tree
 
 // A workgroup of four wavefronts has 32, 64 or 128 rows (a row is a query head of one of the call's rows), which its wavefronts share, 32 each; where fewer wavefronts do, each of
 // them has its part of the entries.  `wide`: wavefronts side by side over rows, 1, 2 or 4.
-CKV_PLAN int rows_tile(int wide) { return wide == 1 ? 2 * kTile : kTile; }
+// The entries that they take at once, 32 each, are a tile.
+CKV_PLAN int rows_tile(int wide) { return 128 / wide; }
 
 // Which entries a block of rows has to look at, in tiles: those of the first `sinks` entries, and those from the oldest that any row's window holds up to the end of the
 // last row's.  Tiles 0 .. first - 1 are the former, from then on those from `base` on.
@@ -50,7 +50,7 @@ CKV_PLAN RowsPlan rows_plan(long long units, int rows, int group, int entries, i
   const int tiles = (int)(((long long)entries + size - 1) / size) + 2;          // sinks and window begin inside a tile
   const long long work = units * p.blocks * tiles, workers = (p.wide == 1 ? 1ll : 2ll) * n_cu;
   long long share = (work + 2 * workers - 1) / (2 * workers);
-  if (share < 4) share = 4;
+  if (share < 4 * p.wide) share = 4 * p.wide;
   p.share = share < tiles ? (int)share : tiles;
   p.places = unit_parts(tiles, p.share);
   p.pieces = units * p.blocks * p.places;
