@@ -1,6 +1,7 @@
 // Host side of the cache in pages (ckv_paged_* in include/ckv.h): argument checks and launches.  Nothing is kept between calls.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "ckv_paged_host.h"
 #include "ckv_paged_kernels.h"
@@ -31,10 +32,10 @@ int check_entries(const ckv_pages* p, const ckv_seqs* s, int n_picked) {
   if ((long long)s->batch * p->n_kv_heads * unit_blocks((int)unit_entries(p, s, n_picked)) > (1ll << 30)) return fail(CKV_EINVAL, "too many entries in all (2^35)");
   return CKV_OK;
 }
-Split split_of(const ckv_pages* p, const ckv_seqs* s, int n_q_heads, int n_picked, int n_cu) {
+Split split_entries(const ckv_pages* p, const ckv_seqs* s, int n_q_heads, int entries, bool same, int n_cu) {
   const long long units = (long long)s->batch * p->n_kv_heads;
   Split r{};
-  r.plan = attend_plan(units, (int)unit_entries(p, s, n_picked), n_picked > 0, n_cu);
+  r.plan = attend_plan(units, entries, same, n_cu);
   if (r.plan.split) {
     const size_t G = (size_t)(n_q_heads / p->n_kv_heads);
     r.partial = up256((size_t)r.plan.pieces * G * kDim * 4);
@@ -43,13 +44,73 @@ Split split_of(const ckv_pages* p, const ckv_seqs* s, int n_q_heads, int n_picke
   }
   return r;
 }
+Split split_of(const ckv_pages* p, const ckv_seqs* s, int n_q_heads, int n_picked, int n_cu) {
+  return split_entries(p, s, n_q_heads, (int)unit_entries(p, s, n_picked), n_picked > 0, n_cu);
+}
+// Of tokens that look back through a window: units whose window is shorter than sequences may be have as much to do each, as a rule.
+Split split_window(const ckv_pages* p, const ckv_seqs* s, int n_q_heads, const ckv_mask* m, int n_cu) {
+  const long long seen = m->window ? 32 * (((long long)m->sinks + 31) / 32 + ((long long)m->window + 31) / 32 + 1) : s->max_length;
+  return split_entries(p, s, n_q_heads, (int)std::min<long long>(seen, s->max_length), m->window > 0 && m->window < s->max_length, n_cu);
+}
 int score_columns(const ckv_pages* p, const ckv_seqs* s) { return (int)(((long long)s->max_length + p->page_size - 1) / p->page_size); }
 size_t score_bytes(const ckv_pages* p, const ckv_seqs* s, int n_cu) {
   const int units = s->batch * p->n_kv_heads, columns = score_columns(p, s);
   return selects_whole(units, columns, n_cu) ? 0 : up256((size_t)units * columns * 4);
 }
 
+// `c`: what is the call's own of pages picked or a window.
+int attend(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_query* query, const Split& s, Attend c, bool window, float scale_log2e, void* out, int32_t out_dtype, float* lse,
+           void* workspace, size_t workspace_bytes, void* stream, const char* what) {
+  const int G = query->n_q_heads / pages->n_kv_heads;
+  if (!launches(s.plan.pieces, kThreads)) return fail(CKV_EINVAL, "too many sequences times KV heads for one attention (2^24)");
+  if (s.bytes() > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < s.bytes())) return fail(CKV_EWORKSPACE, "workspace too small or misaligned");
+  const Paged p = paged_of(pages, seqs);
+  c.q = (const uint8_t*)query->q;
+  c.q_seq_stride = query->seq_stride * 2;
+  c.q_head_stride = query->head_stride * 2;
+  c.out = (uint8_t*)out;
+  c.out_bf16 = out_dtype == CKV_BF16;
+  c.lse = lse;
+  c.partial = (float*)workspace;
+  c.ml = (float*)((char*)workspace + s.partial);
+  c.scale_log2e = scale_log2e;
+  c.G = G;
+  if (s.plan.split) c.parts = (int32_t*)((char*)workspace + s.partial + s.ml);
+  c.share = s.plan.share;
+  c.places = s.plan.places;
+  c.workers = s.plan.workers;
+  const dim3 grid((unsigned)s.plan.pieces);
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, (hipStream_t)stream, p, c); };
+  auto attend = [&](auto windowed) {
+    constexpr bool WINDOW = decltype(windowed)::value;
+    if (pages->dtype == CKV_E4M3) G > 8 ? launch(paged_attend_kernel<true, true, WINDOW>) : launch(paged_attend_kernel<true, false, WINDOW>);
+    else G > 8 ? launch(paged_attend_kernel<false, true, WINDOW>) : launch(paged_attend_kernel<false, false, WINDOW>);
+  };
+  window ? attend(std::true_type()) : attend(std::false_type());
+  if (int rc = launched(what)) return rc;
+  if (!s.plan.split) return CKV_OK;
+  const unsigned units = (unsigned)(seqs->batch * pages->n_kv_heads);
+  const int heads = (int)units > compute_units() ? std::min(G, kJoinRows) : 1;
+  hipLaunchKernelGGL(paged_join_kernel, dim3(units, (unsigned)((G + heads - 1) / heads)), dim3(32 * kJoinRows), 0, (hipStream_t)stream, c, heads);
+  return launched(what);
+}
+
 }  // namespace
+
+namespace ckv {
+size_t one_row_workspace(const ckv_pages* pages, const ckv_seqs* seqs, int n_q_heads, const ckv_mask* mask) {
+  return split_window(pages, seqs, n_q_heads, mask, compute_units()).bytes();
+}
+int attend_one_row(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_query* query, const int32_t* first, const ckv_mask* mask, float scale_log2e, void* out, int32_t out_dtype,
+                   float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  Attend c{};
+  c.first = first;
+  c.window = mask->window;
+  c.sinks = mask->sinks;
+  return attend(pages, seqs, query, split_window(pages, seqs, query->n_q_heads, mask, compute_units()), c, true, scale_log2e, out, out_dtype, lse, workspace, workspace_bytes, stream,
+                "ckv_paged_attend_rows");
+}
+}  // namespace ckv
 
 namespace ckv {
 const char* thread_error() { return t_error; }
@@ -111,39 +172,11 @@ int ckv_paged_attend(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_que
   if (!(softmax_scale > 0.0f) || !std::isfinite(scale_log2e)) return fail(CKV_EINVAL, "softmax_scale must be positive and below 2.3e38");
   if (picked ? n_picked < 1 : n_picked != 0) return fail(CKV_EINVAL, "n_picked must be positive with a list of pages and 0 without");
   if (int rc = check_entries(pages, seqs, n_picked)) return rc;
-  const int G = query->n_q_heads / pages->n_kv_heads;
-  const Split s = split_of(pages, seqs, query->n_q_heads, n_picked, compute_units());
-  if (!launches(s.plan.pieces, kThreads)) return fail(CKV_EINVAL, "too many sequences times KV heads for one attention (2^24)");
-  if (s.bytes() > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < s.bytes())) return fail(CKV_EWORKSPACE, "workspace too small or misaligned");
-  const Paged p = paged_of(pages, seqs);
   Attend c{};
-  c.q = (const uint8_t*)query->q;
-  c.q_seq_stride = query->seq_stride * 2;
-  c.q_head_stride = query->head_stride * 2;
   c.picked = picked;
   c.n_picked = n_picked;
-  c.out = (uint8_t*)out;
-  c.out_bf16 = out_dtype == CKV_BF16;
-  c.lse = lse;
-  c.partial = (float*)workspace;
-  c.ml = (float*)((char*)workspace + s.partial);
-  c.scale_log2e = scale_log2e;
-  c.G = G;
-  if (s.plan.split) c.parts = (int32_t*)((char*)workspace + s.partial + s.ml);
-  c.share = s.plan.share;
-  c.places = s.plan.places;
-  c.workers = s.plan.workers;
-  const dim3 grid((unsigned)s.plan.pieces);
-  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, (hipStream_t)stream, p, c); };
-  const bool wide = G > 8;
-  if (pages->dtype == CKV_E4M3) wide ? launch(paged_attend_kernel<true, true>) : launch(paged_attend_kernel<true, false>);
-  else wide ? launch(paged_attend_kernel<false, true>) : launch(paged_attend_kernel<false, false>);
-  if (int rc = launched("ckv_paged_attend")) return rc;
-  if (!s.plan.split) return CKV_OK;
-  const unsigned units = (unsigned)(seqs->batch * pages->n_kv_heads);
-  const int heads = (int)units > compute_units() ? std::min(G, kJoinRows) : 1;
-  hipLaunchKernelGGL(paged_join_kernel, dim3(units, (unsigned)((G + heads - 1) / heads)), dim3(32 * kJoinRows), 0, (hipStream_t)stream, c, heads);
-  return launched("ckv_paged_attend");
+  return attend(pages, seqs, query, split_of(pages, seqs, query->n_q_heads, n_picked, compute_units()), c, false, scale_log2e, out, out_dtype, lse, workspace, workspace_bytes, stream,
+                "ckv_paged_attend");
 }
 
 int ckv_paged_select(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_query* query, int32_t keep, int32_t keep_first, int32_t keep_last, int32_t* picked,

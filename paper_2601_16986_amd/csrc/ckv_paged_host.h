@@ -139,6 +139,11 @@ inline int compute_units() {
   return n;
 }
 
+// One row of each sequence as ckv_paged_attend_rows takes it (ckv_paged.hip, where the attention of one token is): its workspace, 0 if it needs none, and the call, its arguments checked.
+size_t one_row_workspace(const ckv_pages* pages, const ckv_seqs* seqs, int n_q_heads, const ckv_mask* mask);
+int attend_one_row(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_query* query, const int32_t* first, const ckv_mask* mask, float scale_log2e, void* out, int32_t out_dtype,
+                   float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 constexpr size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 }  // namespace ckv

@@ -4,6 +4,7 @@
 #include <type_traits>
 
 #include "ckv_paged_device.h"
+#include "ckv_rows.h"
 
 namespace ckv {
 
@@ -126,7 +127,31 @@ struct Attend {
   float scale_log2e;
   int32_t G, n_picked, out_bf16;
   int32_t share, places, workers;          // AttendPlan
+  const int32_t* first;      // WINDOW: the tokens' positions, or NULL: the sequences' last
+  int32_t window, sinks;     // WINDOW: entries that a token looks back to, itself included, and first ones
 };
+
+// What one token looks at: all entries of its sequence or, WINDOW, those up to its own position, of which only the last `window` and the first `sinks` count.
+struct Sight {
+  int end, oldest;           // entries oldest .. end - 1, and the first sinks
+  RowTiles blocks;           // in blocks of 32
+};
+template <bool WINDOW>
+__device__ __forceinline__ int sight_end(const Paged& p, const Attend& c, int b, int& bad) {
+  if constexpr (!WINDOW) return p.length(b, bad);
+  p.length(b, bad);
+  const RowSpan s = rows_below(row_span(p.lengths[b], 1, c.first != nullptr, c.first ? c.first[b] : 0, false, 0, 0, 0), p.max_length);
+  if (s.bad) bad |= PAGED_BAD_LENGTH;
+  return s.count ? s.first + 1 : 0;
+}
+template <bool WINDOW>
+__device__ __forceinline__ Sight sight_of(const Attend& c, int end) {
+  if constexpr (!WINDOW) return {end, 0, {0, 0, unit_blocks(end)}};
+  Sight s = {end, c.window && end > c.window ? end - c.window : 0, {}};
+  s.blocks = row_tiles(s.oldest, end, c.sinks, 32);
+  if (s.blocks.count == 0) s.blocks.count = 1;
+  return s;
+}
 
 // Two rows of a pair of entries into pairs of one dimension: word w of the result holds dimension w of both.
 __device__ __forceinline__ void interleave_bytes(uint32_t a, uint32_t b, uint32_t (&x)[2]) {
@@ -142,28 +167,31 @@ __device__ __forceinline__ void put_out(const Attend& c, int64_t row, int d4, f3
 // The piece that a workgroup takes.  Where lengths decide how the work is cut they are only known here, so every workgroup looks for its own; a lane adds up its
 // share of the sequences.  Large pieces come first: the chip's last ones to end are then small.
 struct Piece {
-  int b, h, length, index, first, last, parts, part;      // blocks first .. last - 1 of the unit; piece `index` of all, `part` of the unit's `parts`
+  int b, h, length, index, first, last, parts, part;      // length: the end of what the token sees; blocks first .. last - 1 of the unit; piece `index` of all, `part` of the unit's `parts`
 };
 __device__ __forceinline__ int lane_at(int v, int lane) { return __builtin_amdgcn_ds_bpermute(lane << 2, v); }
+template <bool WINDOW>
 __device__ __forceinline__ bool find_piece(const Paged& p, const Attend& c, int index, int lane, int& bad, Piece& r) {
-  const int fixed = c.picked ? unit_blocks(c.n_picked << p.shift) : 0;
+  const int fixed = !WINDOW && c.picked ? unit_blocks(c.n_picked << p.shift) : 0;
+  auto length_of = [&](int b) { return sight_end<WINDOW>(p, c, b, bad); };
+  auto blocks_of = [&](int length) { return sight_of<WINDOW>(c, length).blocks.count; };
   int n;
   if (c.share) {
     const int u = index / c.places;
     r.part = index - u * c.places;
     r.b = u / p.hkv;
     r.h = u - r.b * p.hkv;
-    r.length = uniform_i32(p.length(r.b, bad));
-    n = fixed ? fixed : unit_blocks(r.length);
+    r.length = uniform_i32(length_of(r.b));
+    n = fixed ? fixed : blocks_of(r.length);
     r.parts = unit_parts(n, c.share);
     if (r.part >= r.parts) return false;
   } else {
     const int per_lane = (p.batch + 63) >> 6, b0 = lane * per_lane;
     int length = 0, blocks = 0, pieces = 0, who = lane;
     for (int i = 0; i < per_lane && b0 + i < p.batch; ++i) {
-      const int m = p.length(b0 + i, bad);
+      const int m = length_of(b0 + i);
       if (i == 0) length = m;
-      blocks += unit_blocks(m);
+      blocks += blocks_of(m);
     }
     int share = attend_share(wave_sum_i32(blocks) * p.hkv, c.workers);
     if (per_lane == 1) {
@@ -183,7 +211,7 @@ __device__ __forceinline__ bool find_piece(const Paged& p, const Attend& c, int 
       pieces = lane_at(pieces, who);
       length = lane_at(length, who);
     } else {
-      for (int i = 0; i < per_lane && b0 + i < p.batch; ++i) pieces += unit_parts(unit_blocks(p.length(b0 + i, bad)), share);
+      for (int i = 0; i < per_lane && b0 + i < p.batch; ++i) pieces += unit_parts(blocks_of(length_of(b0 + i)), share);
     }
     pieces *= p.hkv;
     const int upto = wave_scan_i32(pieces, lane);
@@ -194,11 +222,11 @@ __device__ __forceinline__ bool find_piece(const Paged& p, const Attend& c, int 
     r.b = __builtin_amdgcn_readlane(who, ln) * per_lane;
     r.length = __builtin_amdgcn_readlane(length, ln);
     for (;;) {
-      n = unit_blocks(r.length);
+      n = blocks_of(r.length);
       r.parts = unit_parts(n, share);
       if (index < before + r.parts * p.hkv) break;
       before += r.parts * p.hkv;
-      r.length = uniform_i32(p.length(++r.b, bad));
+      r.length = uniform_i32(length_of(++r.b));
     }
     r.h = (index - before) / r.parts;
     r.part = index - before - r.h * r.parts;
@@ -224,7 +252,7 @@ __device__ __forceinline__ bool find_piece(const Paged& p, const Attend& c, int 
 // without any of the arithmetic, which keeps the vector units busy for a quarter of the time; 16 heads per KV head instead of 4 take 3 % longer, float outputs no longer.  Eight wavefronts per compute unit are enough, and more, or blocks asked
 // for one ahead, only make the streams more: 12 .. 16 of them 202 .. 217 us, 8 KB instead of 4 KB in flight each 191.  A piece costs some 3 us beside its
 // entries (length, page, rows: three trips; joining four wavefronts), so pieces are as few as fill the chip: twice, four, eight times as many 202, 205, 208 us.
-template <bool E4M3, bool WIDE>
+template <bool E4M3, bool WIDE, bool WINDOW = false>
 __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend c) {
   constexpr int kHeads = WIDE ? 16 : 8, kTerms = 3, kWaves = kAttendWaves, kRow = kDim + 4, kParts = E4M3 ? 1 : 2;
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
@@ -232,17 +260,21 @@ __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i32(tid >> 6), j = lane & 15, kg = lane >> 4, shift = p.shift;
   int bad = 0;
   Piece pc;
-  if (!find_piece(p, c, blockIdx.x, lane, bad, pc)) return;
+  if (!find_piece<WINDOW>(p, c, blockIdx.x, lane, bad, pc)) return;
   const int b = pc.b, h = pc.h, u = b * p.hkv + h;
 
   // ---- where the unit's pages lie and how far they are filled, kPageSlots of them at a time, a lane each
-  int page, fill, window = pc.first >> (shift + 1);
+  const Sight sight = sight_of<WINDOW>(c, pc.length);
+  const int oldest = sight.oldest, end = sight.end;
+  auto block = [&](int n) { return WINDOW ? sight.blocks.tile(n) : n; };
+  int page, fill, window = block(pc.first) >> (shift + 1);
   auto look_up = [&]() {
     int logical = window * kPageSlots + lane;
-    if (c.picked) logical = logical < c.n_picked ? c.picked[(int64_t)u * c.n_picked + logical] : -1;
+    if (!WINDOW && c.picked) logical = logical < c.n_picked ? c.picked[(int64_t)u * c.n_picked + logical] : -1;
     page = logical >= 0 && logical < p.columns ? p.table[(int64_t)b * p.table_stride + logical] : 0;      // before the length is there
     fill = logical < 0 || logical >= p.columns ? 0 : page_fill(pc.length, logical, shift);
-    if (c.picked && (logical < -1 || (logical >= 0 && fill == 0))) bad |= PAGED_BAD_PICK;
+    if (WINDOW && fill > 0 && (logical + 1) << shift <= oldest && logical << shift >= c.sinks) fill = 0;         // a page that the token does not look at
+    if (!WINDOW && c.picked && (logical < -1 || (logical >= 0 && fill == 0))) bad |= PAGED_BAD_PICK;
     if (fill > 0 && !page_there(page, p.n_pages)) {
       bad |= PAGED_BAD_PAGE;
       fill = 0;
@@ -267,7 +299,8 @@ __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend 
   for (int dt = 0; dt < 8; ++dt) acc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m_run = kNoLogit, l_run = 0.f;
 
-  for (int blk = pc.first + wave; blk < pc.last; blk += kWaves) {
+  for (int in = pc.first + wave; in < pc.last; in += kWaves) {
+    const int blk = block(in);
     if (blk >> (shift + 1) != window) {
       window = blk >> (shift + 1);
       look_up();
@@ -334,13 +367,13 @@ __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend 
         sv[4 * t + i] = dot[i] * k_scale;
       }
     }
-    // ---- entries that are not there: logits of -inf, values and their scales of nothing (the rows may hold anything)
-    if (valid[0] + valid[1] < 32) {
+    // ---- entries that are not there, or not looked at: logits of -inf, values and their scales of nothing (the rows may hold anything)
+    if (valid[0] + valid[1] < 32 || (WINDOW && blk << 5 < oldest && (blk + 1) << 5 > c.sinks)) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (4 * kg + i >= valid[t]) {
+          if (const int e = (blk << 5) + 16 * t + 4 * kg + i; 4 * kg + i >= valid[t] || (WINDOW && e < oldest && e >= c.sinks)) {
             sv[4 * t + i] = -INFINITY;
             vs[4 * t + i] = 0.f;
             vf[t][i] = u32x4{0u, 0u, 0u, 0u};
@@ -444,7 +477,7 @@ __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend 
         c.ml[2 * at] = M;
         c.ml[2 * at + 1] = L;
       }
-    } else {
+    } else if (!WINDOW || end > 0) {
       const int64_t row = (int64_t)u * c.G + head;
       put_out(c, row, d4, L != 0.f ? y * (1.f / L) : f32x4{0.f, 0.f, 0.f, 0.f});
       if (d4 == 0 && c.lse) c.lse[row] = natural(M, L);

@@ -51,6 +51,11 @@ int check_sizes(const ckv_pages* p, const ckv_seqs* s, int rows, int n_q_heads, 
   return CKV_OK;
 }
 
+// Whether rows are a token of each sequence, without a tree: bound by memory, the attention of one token takes them (unless they are packed, when some sequence may have none).
+bool one_row(const ckv_pages* p, const ckv_seqs* s, int rows, const ckv_mask* m) {
+  return rows == 1 && !m->tree && (long long)s->batch * p->n_kv_heads * unit_blocks(s->max_length) <= (1ll << 30);
+}
+
 // How a call is cut, and what its pieces leave in the workspace.
 struct RowsSplit {
   RowsPlan plan;
@@ -78,7 +83,9 @@ extern "C" {
 
 size_t ckv_paged_rows_workspace_bytes(const ckv_pages* pages, const ckv_seqs* seqs, int32_t rows, int32_t n_q_heads, const ckv_mask* mask) {
   if (check(pages, seqs) != CKV_OK || check_sizes(pages, seqs, rows, n_q_heads, mask) != CKV_OK) return 0;
-  return std::max<size_t>(256, rows_split(pages, seqs, rows, n_q_heads, mask, compute_units()).bytes());
+  size_t bytes = rows_split(pages, seqs, rows, n_q_heads, mask, compute_units()).bytes();
+  if (one_row(pages, seqs, rows, mask)) bytes = std::max(bytes, one_row_workspace(pages, seqs, n_q_heads, mask));
+  return std::max<size_t>(256, bytes);
 }
 
 int ckv_paged_attend_rows(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_row_queries* queries, const ckv_mask* mask, float softmax_scale, void* out,
@@ -92,6 +99,10 @@ int ckv_paged_attend_rows(const ckv_pages* pages, const ckv_seqs* seqs, const ck
   if (seqs->max_length == 0 || (queries->starts && queries->total == 0)) return CKV_OK;
   if (int rc = check_queries(pages, queries)) return rc;
   if (!out || !aligned(out, 16)) return fail(CKV_EINVAL, "out must be a 16-byte aligned device address");
+  if (one_row(pages, seqs, queries->rows, mask) && !queries->starts) {
+    const ckv_query query = {queries->q, queries->seq_stride, queries->head_stride, queries->n_q_heads};
+    return attend_one_row(pages, seqs, &query, queries->first, mask, scale_log2e, out, out_dtype, lse, workspace, workspace_bytes, stream);
+  }
   const RowsSplit s = rows_split(pages, seqs, queries->rows, queries->n_q_heads, mask, compute_units());
   const long long units = (long long)seqs->batch * pages->n_kv_heads, grid = rows_grid(units, (long long)s.plan.blocks * s.plan.places);
   if (!launches(grid, kThreads) || !launches(units * s.plan.blocks, 32 * kRowsJoined)) return fail(CKV_EINVAL, "too many rows for one attention (2^24 blocks of 128, a row per query head)");
@@ -118,7 +129,7 @@ int ckv_paged_attend_rows(const ckv_pages* pages, const ckv_seqs* seqs, const ck
     c.ml = (float*)((char*)workspace + s.partial);
     c.parts = (int32_t*)((char*)workspace + s.partial + s.ml);
   }
-  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), 0, (hipStream_t)stream, p, c); };
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), 0, (hipStream_t)stream, RowsCall{p, c}); };
   auto terms = [&](auto e4m3, auto wide) {
     constexpr bool E4M3 = decltype(e4m3)::value;
     constexpr int WIDE = decltype(wide)::value;
@@ -131,7 +142,7 @@ int ckv_paged_attend_rows(const ckv_pages* pages, const ckv_seqs* seqs, const ck
   if (int rc = launched("ckv_paged_attend_rows")) return rc;
   if (s.plan.places == 1) return CKV_OK;
   const dim3 joins((unsigned)(units * s.plan.blocks), (unsigned)(32 * s.plan.wide / kRowsJoined));
-  auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, joins, dim3(32 * kRowsJoined), 0, (hipStream_t)stream, p, c); };
+  auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, joins, dim3(32 * kRowsJoined), 0, (hipStream_t)stream, RowsCall{p, c}); };
   s.plan.wide == 1 ? join(paged_rows_join_kernel<1>) : s.plan.wide == 2 ? join(paged_rows_join_kernel<2>) : join(paged_rows_join_kernel<4>);
   return launched("ckv_paged_attend_rows");
 }

@@ -29,9 +29,21 @@ struct RowsAttend {
   int32_t blocks, share, places;           // RowsPlan
 };
 
-__device__ __forceinline__ void put_row(const RowsAttend& c, int64_t row, int d4, f32x4 y) {
-  if (c.out_bf16) *reinterpret_cast<u32x2*>(c.out + (row * kDim + d4) * 2) = u32x2{bf16_pack(y[0], y[1]), bf16_pack(y[2], y[3])};
-  else *reinterpret_cast<f32x4*>(c.out + (row * kDim + d4) * 4) = y;
+struct RowsCall {
+  Paged p;
+  RowsAttend c;
+};
+// The kernel's arguments once more, from memory: what is only used now and then does not stay in scalar registers, of which the inner loop needs all (with the arguments in them it kept others
+// in vector registers' lanes, 470 moves a step).
+__device__ __forceinline__ const __attribute__((address_space(4))) RowsCall* args() {
+  auto a = (const __attribute__((address_space(4))) RowsCall*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(a));
+  return a;
+}
+
+__device__ __forceinline__ void put_row(uint8_t* out, bool bf16, int64_t row, int d4, f32x4 y) {
+  if (bf16) *reinterpret_cast<u32x2*>(out + (row * kDim + d4) * 2) = u32x2{bf16_pack(y[0], y[1]), bf16_pack(y[2], y[3])};
+  else *reinterpret_cast<f32x4*>(out + (row * kDim + d4) * 4) = y;
 }
 
 // Lanes l and l + 32 into one value, the same in both.
@@ -60,6 +72,11 @@ __device__ const uint8_t kNothing[256] __attribute__((aligned(16))) = {};       
 typedef __attribute__((address_space(3))) uint8_t lds8;
 __device__ __forceinline__ uint32_t lds_at(const void* p) { return (uint32_t)(uintptr_t)(const lds8*)p; }
 
+__device__ __forceinline__ const uint8_t* uniform_at(const uint8_t* p) {
+  const u64 at = (u64)p;
+  return (const uint8_t*)((u64)(uint32_t)uniform_i32((int)(at >> 32)) << 32 | (uint32_t)uniform_i32((int)at));
+}
+
 // Sixteen bytes of each lane straight into LDS, side by side from `to` on.  The compiler does not know of these loads: told, it takes every read out of LDS for one that may have to
 // wait for them, and waits.  They are waited for by hand (arrived()) before the barrier that lets others read.
 __device__ __forceinline__ void load_to_lds(const uint8_t* from, uint32_t to) {
@@ -68,8 +85,7 @@ __device__ __forceinline__ void load_to_lds(const uint8_t* from, uint32_t to) {
 }
 __device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t lane_at, uint32_t to) {
   to = (uint32_t)uniform_i32((int)to);
-  const u64 at = (u64)base;
-  base = (const uint8_t*)((u64)(uint32_t)uniform_i32((int)(at >> 32)) << 32 | (uint32_t)uniform_i32((int)at));
+  base = uniform_at(base);
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(lane_at), "s"(base) : "memory");
 }
 __device__ __forceinline__ void arrived() { __builtin_amdgcn_s_waitcnt(0x0F70); }          // vmcnt(0)
@@ -101,7 +117,9 @@ struct Rest {
 // nothing, whatever its value: where something that is not finite comes out the piece is done again with the finite values alone, and rows that give others weight
 // get NaN where those are.
 template <bool E4M3, int WIDE, int TERMS>
-__global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel(Paged p, RowsAttend c) {
+__global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel(RowsCall call) {
+  const Paged& p = call.p;
+  const RowsAttend& c = call.c;
   constexpr int kDeep = kAttendWaves / WIDE, kUnit = 32 * kDeep, NU = WIDE == 4 ? 2 : 1, kRows = 32 * WIDE, kBuf = NU * kUnit * 256;
   constexpr int kLoads = kUnit / (E4M3 ? 32 : 16), kWords = kMaxDrafts / 32 + 3;
   __shared__ __align__(16) uint8_t s_tile[2][2][kBuf];          // keys, values; two buffers of NU units each
@@ -110,6 +128,7 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
   __shared__ int s_odd;
   static_assert(sizeof s_tile >= kAttendWaves * 32 * kDim * 4, "the outputs go where the tiles were");
 
+  if (threadIdx.x == 0) s_odd = 0;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i32(tid >> 6), j = lane & 31, half = lane >> 5, wq = wave % WIDE, wk = wave / WIDE;
   const int64_t each = (int64_t)c.blocks * c.places, piece = rows_piece(blockIdx.x, c.units, each);
   if (piece < 0) return;
@@ -181,103 +200,144 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
   }
   f32x16 acc[4];
   float m_run, l_run;
+  const float scale_log2e = c.scale_log2e;
 
   // ---- units' way into LDS: rows of 256 bytes, bf16 straight there, 8 bits through registers
   const int units = n_last - n_first;
   auto unit_at = [&](int i) CKV_INLINE { return tiles.tile(n_first + i) * kUnit; };
   auto seen = [&](int e) CKV_INLINE { return e < end && (e >= oldest || e < sinks); };
-  int missing = 0;                               // a page that some row needs and that is not there
-  // Where kPageSlots pages lie, a lane each: of the sequence's pages kPageSlots * window and on (page -1 where there is none, and the place of the pool's first).
+  // Where kPageSlots pages lie, a lane each, of the sequence's pages kPageSlots * window and on, and the ones before them (the pool's first instead of one that is not there).
   struct Known {
-    int window = -1, page = -1;
-    u64 at = 0ull;
-  } k_known, v_known;
+    int window = -1;
+    u64 row = 0ull, scale = 0ull;
+  } known, before;
   u32x4 kr[E4M3 ? NU * kLoads : 1], vr[E4M3 ? NU * kLoads : 1];
   uint32_t ks[E4M3 ? NU * kLoads : 1], vs[E4M3 ? NU * kLoads : 1];
-  const int r_in = E4M3 ? tid >> 3 : tid >> 4;   // the thread's row of those that a load takes
-  const uint32_t lane_at = (uint32_t)((E4M3 ? r_in & 15 : r_in) * p.slot_stride + 16 * (E4M3 ? tid & 7 : (tid & 15) ^ swizzle(r_in)));
+  constexpr int kOnce = E4M3 ? 32 : 16;          // rows of a load
+  const int r_in = tid / (kThreads / kOnce);     // the thread's
   const int shift = p.shift, page_mask = p.page_size() - 1, slot_stride = p.slot_stride;
-  auto look_up = [&](int e0, const uint8_t* pool, Known& known) CKV_INLINE {
-    const int w = (e0 >> shift) / kPageSlots;
-    if (w == known.window) return;
-    known.window = w;
-    const int64_t logical = (int64_t)w * kPageSlots + lane, from = logical << shift, upto = from + page_mask + 1;
-    const bool needed = logical < p.columns && from < end && (upto > oldest || from < sinks);
-    const int page = needed ? p.table[(int64_t)b * p.table_stride + logical] : -1;
-    const bool there = page_there(page, p.n_pages);
+  const uint32_t in_row = 16 * (E4M3 ? tid & 7 : (tid & 15) ^ swizzle(r_in)), lane_at = (uint32_t)(r_in * slot_stride) + in_row, next_at = lane_at + (uint32_t)(kOnce * slot_stride);
+  const u64 k_to_v = (u64)p.v - (u64)p.k;
+  auto pages = [&](int logical, Known& to) CKV_INLINE {
+    const auto a = args();
+    const int64_t from = (int64_t)logical << shift, upto = from + page_mask + 1;
+    const bool needed = logical < a->p.columns && from < end && (upto > oldest || from < sinks);
+    const int page = needed ? a->p.table[(int64_t)b * a->p.table_stride + logical] : -1;
+    const bool there = page_there(page, a->p.n_pages);
     if (needed && !there) bad |= PAGED_BAD_PAGE;
-    missing |= __ballot(needed && !there) != 0ull;
-    known.page = there ? page : -1;
-    known.at = (u64)(pool + (there ? page : 0) * p.page_stride + h * p.head_stride);
+    if (__ballot(needed && !there) != 0ull) s_odd = 1;           // once more, with care
+    to.row = (u64)(a->p.k + (there ? page : 0) * a->p.page_stride + h * a->p.head_stride);
+    if constexpr (E4M3) to.scale = (u64)(a->p.scales + (there ? page : 0) * a->p.scale_page_stride + h * a->p.scale_head_stride);
   };
-  // The unit's entries from e0 on.  ALL: every one is there and seen; otherwise those that no row of the block sees, or that have no page, come as zeros: whatever lies there times a weight of
-  // nothing must be nothing.
-  auto ask_side = [&](auto all_, int e0, const Known& known, uint32_t to, u32x4* rr, uint32_t* ss, int side) CKV_INLINE {
-    constexpr bool ALL = decltype(all_)::value;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int e = e0 + (E4M3 ? 32 * i + 16 * (wave >> 1) : 16 * i), off = e & page_mask, slot = (e >> shift) & (kPageSlots - 1);
-      const uint8_t* from = (const uint8_t*)readlane_u64(known.at, slot) + (uint32_t)(off * slot_stride);
-      if constexpr (E4M3) {
-        const int page = __builtin_amdgcn_readlane(known.page, slot);
-        rr[i] = load16(from + lane_at);
-        ss[i] = p.scales[max(page, 0) * p.scale_page_stride + h * p.scale_head_stride + 2 * (off + (r_in & 15)) + side];
-        if (!ALL) {
-          apart();
-          if (page < 0 || !seen(e + (r_in & 15))) rr[i] = u32x4{0u, 0u, 0u, 0u}, ss[i] = 127u;
-        }
-      } else if (ALL) {
-        load_to_lds(from, lane_at, to + (16 * i + 4 * wave) * 256);
-      } else {
-        const int page = __builtin_amdgcn_readlane(known.page, slot);
-        load_to_lds(page >= 0 && seen(e + r_in) ? from + lane_at : kNothing + 16 * (tid & 15), to + (16 * i + 4 * wave) * 256);
-      }
-    }
+  auto of_slot = [&](u64 v, int slot) CKV_INLINE {
+    const uint32_t x = (uint32_t)__builtin_amdgcn_ds_bpermute(slot << 2, (int)(uint32_t)v), z = (uint32_t)__builtin_amdgcn_ds_bpermute(slot << 2, (int)(uint32_t)(v >> 32));
+    return (u64)z << 32 | x;
   };
   const uint32_t k_lds = lds_at(&s_tile[0][0][0]), v_lds = lds_at(&s_tile[1][0][0]);
-  // The n-th buffers: keys of units NU n + 1 and on, values of units NU n - 1 and on.
-  auto ask = [&](int n, int buf) CKV_INLINE {
-#pragma unroll 1
-    for (int s = 0; s < NU; ++s) {
-      const int k = NU * n + 1 + s, v = NU * n - 1 + s;
-      const uint32_t to = buf * kBuf + s * kUnit * 256;
-      auto side = [&](int unit, const uint8_t* pool, Known& known, uint32_t lds, u32x4* rr, uint32_t* ss, int which) CKV_INLINE {
-        if (unit < 0 || unit >= units) return;
-        const int e0 = unit_at(unit);
-        look_up(e0, pool, known);
-        ask_side(std::false_type(), e0, known, lds + to, rr, ss, which);
-      };
-      if constexpr (E4M3 && NU == 2) {            // registers by their names
-        if (s == 0) {
-          side(k, p.k, k_known, k_lds, kr, ks, 0);
-          side(v, p.v, v_known, v_lds, vr, vs, 1);
-        } else {
-          side(k, p.k, k_known, k_lds, kr + kLoads, ks + kLoads, 0);
-          side(v, p.v, v_known, v_lds, vr + kLoads, vs + kLoads, 1);
-        }
-      } else {
-        side(k, p.k, k_known, k_lds, kr, ks, 0);
-        side(v, p.v, v_known, v_lds, vr, vs, 1);
-      }
-    }
-  };
-  auto ask_steady = [&](int buf, int e0) CKV_INLINE {          // values from e0 on, keys two units behind them
+
+  // The n-th buffers take keys of units NU n + 1 and on, values of units NU n - 1 and on.  The easy way, while units' entries follow one another, each unit in one page of those that are known, all of
+  // them seen by some row: a page's place out of its lane, and values where the keys of two units before were.  Units below `easy`, from `plain` on (values), may go it.
+  int easy = 0, plain = 0;
+  struct Rows4 {
+    u64 k_row[NU], k_scale[NU];
+  } last = {}, last2 = {};         // of the units whose keys were asked for last, and before that
+  uint32_t unseen = 0u;
+  // 8 bits go into registers, with no branch around their loads: loaded registers would be copied where ways meet, and waited for.  So the ways only work out places.
+  u64 at[E4M3 ? 2 : 1][E4M3 ? NU * kLoads : 1], scale_of[E4M3 ? 2 : 1][E4M3 ? NU * kLoads : 1];
+  auto ask_easy = [&](int n, int buf) CKV_INLINE {
+    Rows4 now;
+    const Rows4& v_last = NU == 2 ? last : last2;
+    const int e0 = unit_at(NU * n + 1);
 #pragma unroll
     for (int s = 0; s < NU; ++s) {
-      const uint32_t to = buf * kBuf + s * kUnit * 256;
-      look_up(e0 + (2 + s) * kUnit, p.k, k_known);
-      look_up(e0 + s * kUnit, p.v, v_known);
-      ask_side(std::true_type(), e0 + (2 + s) * kUnit, k_known, k_lds + to, &kr[E4M3 ? s * kLoads : 0], &ks[E4M3 ? s * kLoads : 0], 0);
-      ask_side(std::true_type(), e0 + s * kUnit, v_known, v_lds + to, &vr[E4M3 ? s * kLoads : 0], &vs[E4M3 ? s * kLoads : 0], 1);
+      const int e = e0 + s * kUnit, slot = (e >> shift) & (kPageSlots - 1), off = e & page_mask;
+      now.k_row[s] = readlane_u64(known.row, slot) + (uint32_t)(off * slot_stride);
+      if constexpr (E4M3) now.k_scale[s] = readlane_u64(known.scale, slot) + (uint32_t)(2 * off);
+#pragma unroll
+      for (int side = 0; side < 2; ++side) {
+        u64 row = side ? v_last.k_row[s] + k_to_v : now.k_row[s];
+        const u64 scale = side ? v_last.k_scale[s] + 1 : now.k_scale[s];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          if constexpr (E4M3) {
+            at[side][s * kLoads + i] = row + (i & 1 ? next_at : lane_at);
+            scale_of[side][s * kLoads + i] = scale + (uint32_t)(2 * (kOnce * i + r_in));
+          } else {
+            load_to_lds((const uint8_t*)row, i & 1 ? next_at : lane_at, (side ? v_lds : k_lds) + buf * kBuf + s * kUnit * 256 + (16 * i + 4 * wave) * 256);
+          }
+          if (i & 1) row += (uint32_t)(2 * kOnce * slot_stride);
+        }
+      }
     }
+    last2 = last;
+    last = now;
   };
-  auto ask_next = [&](int n, int buf) CKV_INLINE {             // the one where it can be, or the other
-    const int v = NU * n - 1, k = NU * n + NU, e0 = unit_at(v), e1 = e0 + (NU + 2) * kUnit - 1;
-    if (k < units && unit_at(k) + kUnit - 1 == e1 && e0 >= oldest && e1 < end && !missing) ask_steady(buf, e0);
-    else ask(n, buf);
+  // Any way: every lane by the place of its own row.  Values of entries that no row of the block sees come as zeros: whatever lies there times a weight of nothing must be nothing (of keys it does not
+  // matter).
+  auto ask_any = [&](int n, int buf) CKV_INLINE {
+    apart();
+    last2 = last;
+#pragma unroll
+    for (int s = 0; s < NU; ++s)
+#pragma unroll
+      for (int side = 0; side < 2; ++side) {
+        const int unit = NU * n + (side ? -1 : 1) + s, e0 = unit_at(min(max(unit, 0), units - 1)), w = (e0 >> shift) / kPageSlots;
+        const bool all = unit >= 0 && unit < units && e0 >= oldest && e0 + kUnit <= end;
+        Known from;
+        if (side == 0) {
+          if (w != known.window) {
+            before = known;
+            known.window = w;
+            pages(w * kPageSlots + lane, known);
+          }
+          from = known;
+          if (!all) plain = unit + 1;
+          const int left = min((w + 1) * kPageSlots << shift, end) - e0, slot = (e0 >> shift) & (kPageSlots - 1), off = e0 & page_mask;
+          easy = all && page_mask + 1 >= kUnit && n_first + unit >= tiles.sinks ? min(units, unit + left / kUnit) : 0;
+          last.k_row[s] = readlane_u64(known.row, slot) + (uint32_t)(off * slot_stride);
+          if constexpr (E4M3) last.k_scale[s] = readlane_u64(known.scale, slot) + (uint32_t)(2 * off);
+        } else {
+          from.row = w == known.window ? known.row : before.row;
+          from.scale = w == known.window ? known.scale : before.scale;
+          if (w != known.window && w != before.window) pages(w * kPageSlots + lane, from);
+        }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          const int e = e0 + kOnce * i + r_in, slot = (e >> shift) & (kPageSlots - 1), off = e & page_mask;
+          const u64 row = of_slot(from.row, slot) + (side ? k_to_v : 0ull) + (uint32_t)(off * slot_stride) + in_row;
+          if constexpr (E4M3) {
+            at[side][s * kLoads + i] = row;
+            scale_of[side][s * kLoads + i] = of_slot(from.scale, slot) + (uint32_t)(2 * off + side);
+            if (side && !(unit >= 0 && unit < units && seen(e))) unseen |= 1u << (s * kLoads + i);
+          } else {
+            const uint32_t to = (side ? v_lds : k_lds) + buf * kBuf + s * kUnit * 256 + (16 * i + 4 * wave) * 256;
+            load_to_lds(!side || (unit >= 0 && unit < units && seen(e)) ? (const uint8_t*)row : kNothing + 16 * (tid & 15), to);
+          }
+        }
+      }
+  };
+  auto ask = [&](auto easy_, int n, int buf) CKV_INLINE {
+    unseen = 0u;
+    if (decltype(easy_)::value && NU * n + NU < easy && NU * n - 1 >= plain) ask_easy(n, buf);
+    else ask_any(n, buf);
+    if constexpr (E4M3) {
+#pragma unroll
+      for (int i = 0; i < NU * kLoads; ++i) {
+        kr[i] = load16((const uint8_t*)at[0][i]);
+        ks[i] = *(const uint8_t*)scale_of[0][i];
+        vr[i] = load16((const uint8_t*)at[1][i]);
+        vs[i] = *(const uint8_t*)scale_of[1][i];
+      }
+    }
   };
   auto put = [&](int buf) CKV_INLINE {
     if constexpr (E4M3) {
+      if (__any(unseen != 0u)) {
+        apart();
+#pragma unroll
+        for (int i = 0; i < NU * kLoads; ++i)
+          if (unseen >> i & 1u) vr[i] = u32x4{0u, 0u, 0u, 0u}, vs[i] = 127u;
+      }
 #pragma unroll
       for (int i = 0; i < NU * kLoads; ++i) {
         const float a = __uint_as_float(ks[i] << 23), z = __uint_as_float(vs[i] << 23);
@@ -295,17 +355,22 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
   };
 
   // ---- one unit after another: the weights of one, the outputs of the one before, the logits of the one behind
-  uint32_t ka[8], va[4], vz[4];                  // where a lane reads keys of 16 dimensions, and 4 + 4 values of 32
-#pragma unroll
-  for (int x = 0; x < 8; ++x) ka[x] = k_lds + (wk * 32 + j) * 256 + (((2 * x + half) ^ swizzle(j)) << 4);
-  {
-    const int l16 = lane & 15, at = (4 * half + (l16 >> 2)) * 256 + (l16 & 1) * 8 + (((((lane >> 4) & 1) * 2 + ((l16 >> 1) & 1)) ^ half) << 4);
-#pragma unroll
-    for (int d = 0; d < 4; ++d) {
-      va[d] = v_lds + wk * 32 * 256 + (at ^ (((l16 >> 2) ^ d) << 6));
-      vz[d] = v_lds + wk * 32 * 256 + (at ^ (((l16 >> 2) ^ d) << 6) ^ 32) + 8 * 256;
-    }
-  }
+  // where a lane reads keys of the first 16 dimensions, and values of the first 32: of others at that ^ 32 x, that ^ 64 d; the other four of its eight entries at that ^ 32, eight rows on
+  uint32_t k_at_ = k_lds + (wk * 32 + j) * 256 + ((half ^ swizzle(j)) << 4);
+  const int l16 = lane & 15;
+  uint32_t v_at_ = v_lds + (wk * 32 + 4 * half + (l16 >> 2)) * 256 + ((l16 >> 2) << 6 | ((((lane >> 4) & 1) * 2 + ((l16 >> 1) & 1)) ^ half) << 4 | (l16 & 1) * 8);
+  // (With registers that 8 bits need on their way these places are worked out again and again, not kept.)
+  auto keys = [&](int x, int at) CKV_INLINE {
+    uint32_t k_at = k_at_;
+    if constexpr (E4M3) here(k_at);
+    return read_row(k_at ^ 32 * x, at);
+  };
+  auto values = [&](int n, int at, s16x4 (&v)[2]) CKV_INLINE {                       // n = 2 d + x: dimensions 32 d and on, entries 16 x and on
+    uint32_t v_at = v_at_;
+    if constexpr (E4M3) here(v_at);
+    v[0] = read_transposed(v_at ^ 64 * (n >> 1), at + (n & 1) * 16 * 256);
+    v[1] = read_transposed(v_at ^ (64 * (n >> 1) + 32), at + (n & 1) * 16 * 256 + 8 * 256);
+  };
   auto product = [](s16x8 a, u32x4 w, f32x16 c) CKV_INLINE { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, w), c, 0, 0, 0); };
   auto logits = [&](u32x4 k, int x, f32x16 c) CKV_INLINE { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), q[x], c, 0, 0, 0); };
   f32x16 nought;
@@ -318,7 +383,7 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
     float bm = max3(s[0], s[1], s[2]);
 #pragma unroll
     for (int i = 3; i < 15; i += 2) bm = max3(bm, s[i], s[i + 1]);
-    bm = halves_combine(max2(bm, s[15]), [](float x, float y) { return max2(x, y); }) * c.scale_log2e;
+    bm = halves_combine(max2(bm, s[15]), [](float x, float y) { return max2(x, y); }) * scale_log2e;
     return bm > m_run + kSlack ? bm : m_run;
   };
   auto shrink_by = [&](float f) CKV_INLINE {
@@ -328,12 +393,46 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[d][i] *= f;
   };
-  // A unit in the middle of many, all of it seen by all of the wavefront's rows: products, and what else there is to do, in turn, so that neither waits for the other.
-  auto steady = [&](auto at_, f32x16& s, f32x16& t, u32x4 (&w)[TERMS][2], u32x4 (&y)[TERMS][2]) CKV_INLINE {
+  // Whether `count` units from the i-th on are there, side by side, and seen whole by all of the wavefront's rows.
+  auto clear = [&](int i, int count) CKV_INLINE {
+    const int e0 = unit_at(i), e1 = unit_at(i + count - 1) + kUnit;
+    return (bool)((i + count <= units) & (e1 - e0 == count * kUnit) & (e1 <= wave_hi) & ((e0 >= wave_lo) | (e1 <= sinks)));
+  };
+  // Logits of entries that a row does not see: -inf.
+  auto mask = [&](auto careful_, int i, f32x16& s) CKV_INLINE {
+    apart();
+    const int e_first = unit_at(min(i, units - 1)) + wk * 32, e_last = e_first + 31;
+    uint32_t sees = 0u;
+    const auto a = args();
+    if (valid && i < units) {
+      sees = (uint32_t)bits_between(e_first, lo, hi) | (uint32_t)bits_between(e_first, 0, min(sinks, hi));
+      if (a->c.tree && e_last >= first) {
+        const uint32_t* bits = s_see[token - t_lo];
+        const int from = e_first - first, word = max(from, 0) >> 5, by = max(from, 0) & 31;
+        const uint32_t drafts = (uint32_t)(((u64)bits[word + 1] << 32 | bits[word]) >> by);
+        sees |= from >= 0 ? drafts : drafts << -from;
+      }
+    }
+    if constexpr (decltype(careful_)::value) {
+      for (int x = 0; x < 2; ++x) {
+        const int col = (e_first + 16 * x) >> shift;
+        if (col >= a->p.columns || !page_there(a->p.table[(int64_t)b * a->p.table_stride + col], a->p.n_pages)) sees &= ~(0xFFFFu << 16 * x);
+      }
+    }
+    sees >>= 4 * half;
+#pragma unroll
+    for (int x = 0; x < 16; ++x)
+      if (!(sees >> (8 * (x >> 2) + (x & 3)) & 1u)) s[x] = -INFINITY;
+  };
+  // The step of the i-th unit: products, and what else there is to do, in turn, so that neither waits for the other.
+  auto steady = [&](auto at_, int i, bool whole, f32x16& s, f32x16& t, u32x4 (&w)[TERMS][2], u32x4 (&y)[TERMS][2]) CKV_INLINE {
     constexpr int at = decltype(at_)::value;
-    u32x4 ko[2] = {read_row(ka[0], at), read_row(ka[1], at)};
-    s16x4 vo[2][2] = {{read_transposed(va[0], at), read_transposed(vz[0], at)}, {read_transposed(va[0], at + 16 * 256), read_transposed(vz[0], at + 16 * 256)}};
+    u32x4 ko[2] = {keys(0, at), keys(1, at)};
+    s16x4 vo[2][2];
+    values(0, at, vo[0]);
+    values(1, at, vo[1]);
     const Rest rest;
+    if (!whole) mask(std::false_type(), i, s);
     const float m = grown(s), f = fast_exp2(m_run - m);
     float sum = 0.f, a = 0.f, z = 0.f;
     // the last term of a pair is taken a step later: what a sum of products leaves can be read only some instructions on
@@ -347,13 +446,13 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
     for (int n = 0; n < 8; ++n) {
       t = logits(ko[n & 1], n, n ? t : nought);
       const float a_last = a, z_last = z;
-      a = fmaf(s[2 * n], c.scale_log2e, -m), z = fmaf(s[2 * n + 1], c.scale_log2e, -m);
+      a = fmaf(s[2 * n], scale_log2e, -m), z = fmaf(s[2 * n + 1], scale_log2e, -m);
       here(a);
       here(z);
       a = fast_exp2(a);
       here(a);
       if (n) last(n - 1, a_last, z_last);
-      if (n < 6) ko[n & 1] = read_row(ka[n + 2], at);
+      if (n < 6) ko[n & 1] = keys(n + 2, at);
       fence();
       const s16x8 v = beside(vo[n & 1][0], vo[n & 1][1]);
       acc[n >> 1] = product(v, w[0][n & 1], acc[n >> 1]);
@@ -372,10 +471,7 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
         rest(pair, a, z);
         here(a);
         here(z);
-        if (x == 1 && n < 6) {
-          vo[n & 1][0] = read_transposed(va[(n + 2) >> 1], at + (n & 1) * 16 * 256);
-          vo[n & 1][1] = read_transposed(vz[(n + 2) >> 1], at + (n & 1) * 16 * 256);
-        }
+        if (x == 1 && n < 6) values(n + 2, at, vo[n & 1]);
         fence();
       }
     }
@@ -389,17 +485,18 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
   };
   f32x16 s, t;
   u32x4 w[TERMS][2], y[TERMS][2];
-  // Any unit.
-  auto any = [&](int careful, int i, int at) CKV_INLINE {
+  // The same with care: a unit's values that are not finite reach those rows only that give them weight.
+  auto any = [&](int i, int at) CKV_INLINE {
     if (i >= 1 && i <= units) {
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
         f32x16 wrong = nought;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          s16x8 v = beside(read_transposed(va[d] + at, x * 16 * 256), read_transposed(vz[d] + at, x * 16 * 256));
-          if (careful) {
-            apart();
+          s16x4 vo[2];
+          values(2 * d + x, at, vo);
+          s16x8 v = beside(vo[0], vo[1]);
+          {
             s16x8 ones;
             u32x4 weight;
 #pragma unroll
@@ -415,37 +512,13 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
 #pragma unroll
           for (int n = 0; n < TERMS; ++n) acc[d] = product(v, w[n][x], acc[d]);
         }
-        if (careful) {
-          apart();
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (wrong[e] != 0.f) acc[d][e] = NAN;
-        }
+        for (int e = 0; e < 16; ++e)
+          if (wrong[e] != 0.f) acc[d][e] = NAN;
       }
     }
     if (i >= 0 && i < units) {
-      const int e_first = unit_at(i) + wk * 32, e_last = e_first + 31;
-      if (missing || e_last >= wave_hi || (e_first < wave_lo && e_last >= sinks)) {
-        apart();
-        uint32_t sees = 0u;
-        if (valid) {
-          sees = (uint32_t)bits_between(e_first, lo, hi) | (uint32_t)bits_between(e_first, 0, min(sinks, hi));
-          if (c.tree && e_last >= first) {
-            const uint32_t* bits = s_see[token - t_lo];
-            const int from = e_first - first, word = max(from, 0) >> 5, by = max(from, 0) & 31;
-            const uint32_t drafts = (uint32_t)(((u64)bits[word + 1] << 32 | bits[word]) >> by);
-            sees |= from >= 0 ? drafts : drafts << -from;
-          }
-        }
-        for (int x = 0; missing && x < 2; ++x) {
-          const int col = (e_first + 16 * x) >> p.shift;
-          if (col >= p.columns || !page_there(p.table[(int64_t)b * p.table_stride + col], p.n_pages)) sees &= ~(0xFFFFu << 16 * x);
-        }
-        sees >>= 4 * half;
-#pragma unroll
-        for (int x = 0; x < 16; ++x)
-          if (!(sees >> (8 * (x >> 2) + (x & 3)) & 1u)) s[x] = -INFINITY;
-      }
+      mask(std::true_type(), i, s);
       const float m = grown(s);
       if (__any(m > m_run)) {
         apart();
@@ -456,7 +529,7 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
       float sum = 0.f;
 #pragma unroll
       for (int n = 0; n < 8; ++n) {
-        float a = fast_exp2(fmaf(s[2 * n], c.scale_log2e, -m)), z = fast_exp2(fmaf(s[2 * n + 1], c.scale_log2e, -m));
+        float a = fast_exp2(fmaf(s[2 * n], scale_log2e, -m)), z = fast_exp2(fmaf(s[2 * n + 1], scale_log2e, -m));
         sum += a;
         sum += z;
 #pragma unroll
@@ -469,68 +542,66 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
     }
     if (i + 1 >= 0 && i + 1 < units) {
 #pragma unroll
-      for (int x = 0; x < 8; ++x) s = logits(read_row(ka[x] + at, 0), x, x ? s : nought);
+      for (int x = 0; x < 8; ++x) s = logits(keys(x, at), x, x ? s : nought);
     }
   };
-  if (tid == 0) s_odd = 0;
-  for (int careful = 0;; careful = 1) {
+  const uint32_t k_at0 = k_at_, v_at0 = v_at_;
+  auto begin = [&]() CKV_INLINE {
 #pragma unroll
     for (int d = 0; d < 4; ++d) acc[d] = nought;
     m_run = kNoLogit, l_run = 0.f;
-    const int n_end = units / NU;
-    ask(-1, 1);
+    known.window = before.window = -1;
+    ask(std::false_type(), -1, 1);
     put(1);
-    for (int n = -1; n <= n_end;) {
-      // 2 NU units from the n-th buffers' on, which are those of 0 and 1
-      const int i = NU * n;
-      if ((n & 1) == 0 && i >= 1 && i + 2 * NU < units && !(missing | careful)) {
-        const int e0 = unit_at(i), e1 = e0 + 2 * NU * kUnit - 1;
-        if (unit_at(i + 2 * NU - 1) + kUnit - 1 == e1 && e1 < wave_hi && e0 >= wave_lo) {
-          ask_next(n + 1, 1);
-          steady(std::integral_constant<int, 0>(), s, t, w, y);
-          if constexpr (NU == 2) steady(std::integral_constant<int, kUnit * 256>(), t, s, y, w);
-          put(1);
-          if (missing) {            // a page of those just asked for
-            apart();
-            if constexpr (NU == 1) {
-              s = t;
+  };
+  __syncthreads();                               // s_odd
+  begin();
+  ask(std::false_type(), 0, 0);
+  k_at_ += kBuf, v_at_ += kBuf;
 #pragma unroll
-              for (int x = 0; x < TERMS; ++x) w[x][0] = y[x][0], w[x][1] = y[x][1];
-            }
-            ++n;
-            continue;
-          }
-          ask_next(n + 2, 0);
-          if constexpr (NU == 2) {
-            steady(std::integral_constant<int, kBuf>(), s, t, w, y);
-            steady(std::integral_constant<int, kBuf + kUnit * 256>(), t, s, y, w);
-          } else {
-            steady(std::integral_constant<int, kBuf>(), t, s, y, w);
-          }
-          put(0);
-          n += 2;
-          continue;
-        }
-      }
-      const int buf = n & 1;
-      if (n < n_end) ask(n + 1, buf ^ 1);
-#pragma unroll 1
-      for (int x = 0; x < NU; ++x) any(careful, i + x, buf * kBuf + x * kUnit * 256);
-      if (n < n_end) put(buf ^ 1);
-      ++n;
+  for (int x = 0; x < 8; ++x) s = logits(keys(x, (NU - 1) * kUnit * 256), x, x ? s : nought);
+#pragma unroll
+  for (int x = 0; x < TERMS; ++x) w[x][0] = w[x][1] = u32x4{0u, 0u, 0u, 0u};
+  put(0);
+  // The n-th step, of NU units, works on the buffers of n & 1, while the next ones are filled.
+  for (int n = 0;; ++n) {
+    const int buf = n & 1, i = NU * n;
+    if (i + NU <= units) ask(std::true_type(), n + 1, buf ^ 1);
+    k_at_ += buf ? kBuf : -kBuf;
+    v_at_ += buf ? kBuf : -kBuf;
+    const bool whole = clear(i, NU);
+    steady(std::integral_constant<int, 0>(), i, whole, s, t, w, y);
+    if constexpr (NU == 2) {
+      steady(std::integral_constant<int, kUnit * 256>(), i + 1, whole, t, s, y, w);
+    } else {
+      s = t;
+#pragma unroll
+      for (int x = 0; x < TERMS; ++x) w[x][0] = y[x][0], w[x][1] = y[x][1];
     }
-    __syncthreads();
-    // Once more with care where something that is no number came out: a value that only some rows see must not reach the others.
-    if (careful) break;
-    float nothing = 0.f;
+    if (i + NU > units) break;
+    put(buf ^ 1);
+  }
+  __syncthreads();
+  // Once more with care where a page was missing, or something that is no number came out: a value that only some rows see must not reach the others.
+  float nothing = 0.f;
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
+  for (int d = 0; d < 4; ++d)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) nothing = fmaf(acc[d][i], 0.f, nothing);
-    if (!(nothing == 0.f)) s_odd = 1;
-    __syncthreads();
-    if (!uniform_i32(s_odd)) break;
-    k_known.window = v_known.window = -1;
+    for (int i = 0; i < 16; ++i) nothing = fmaf(acc[d][i], 0.f, nothing);
+  if (!(nothing == 0.f)) s_odd = 1;
+  __syncthreads();
+  if (uniform_i32(s_odd)) {
+    apart();
+    begin();
+    k_at_ = k_at0, v_at_ = v_at0;
+#pragma unroll 1
+    for (int n = -1; NU * n <= units; ++n) {
+      const int buf = n & 1;
+      ask(std::false_type(), n + 1, buf ^ 1);
+#pragma unroll 1
+      for (int x = 0; x < NU; ++x) any(NU * n + x, buf * kBuf + x * kUnit * 256);
+      put(buf ^ 1);
+    }
   }
 
   // ---- the wavefronts' states into one
@@ -543,7 +614,10 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
     for (int a = 0; a < 4; ++a)
       *reinterpret_cast<f32x4*>(s_o + (wave * 32 + j) * kDim + 4 * ((8 * d + 2 * a + half) ^ j)) = f32x4{acc[d][4 * a], acc[d][4 * a + 1], acc[d][4 * a + 2], acc[d][4 * a + 3]};
   __syncthreads();
-  const int64_t out_row = c.rows.starts ? c.rows.starts[b] : (int64_t)b * c.rows.rows;
+  const auto a = args();
+  const int G = a->c.G, hkv = a->p.hkv;
+  const int64_t out_row = a->c.rows.starts ? a->c.rows.starts[b] : (int64_t)b * a->c.rows.rows;
+  float* lse = a->c.lse;
   for (int x = tid; x < kRows * (kDim / 4); x += kThreads) {
     const int r = x >> 5, chunk = x & 31, in = r & 31;
     if (r0 + r >= n_rows) break;
@@ -559,23 +633,25 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
       y += *reinterpret_cast<const f32x4*>(s_o + (w * 32 + in) * kDim + 4 * (chunk ^ in)) * f;
     }
     if (parts > 1) {
-      const int64_t at = (block_index * c.places + part) * kRows + r;
-      *reinterpret_cast<f32x4*>(c.partial + at * kDim + 4 * chunk) = y;
-      if (chunk == 0) c.ml[2 * at] = M, c.ml[2 * at + 1] = L;
+      const int64_t at = (block_index * a->c.places + part) * kRows + r;
+      *reinterpret_cast<f32x4*>(a->c.partial + at * kDim + 4 * chunk) = y;
+      if (chunk == 0) a->c.ml[2 * at] = M, a->c.ml[2 * at + 1] = L;
     } else {
-      const int t = (int)((r0 + r) / c.G);
-      const int64_t to = (out_row + t) * (c.G * p.hkv) + h * c.G + (int)(r0 + r - (uint32_t)t * c.G);
-      put_row(c, to, 4 * chunk, L != 0.f ? y * (1.f / L) : f32x4{0.f, 0.f, 0.f, 0.f});
-      if (chunk == 0 && c.lse) c.lse[to] = natural(M, L);
+      const int t = (int)((r0 + r) / G);
+      const int64_t to = (out_row + t) * (G * hkv) + h * G + (int)(r0 + r - (uint32_t)t * G);
+      put_row(a->c.out, a->c.out_bf16, to, 4 * chunk, L != 0.f ? y * (1.f / L) : f32x4{0.f, 0.f, 0.f, 0.f});
+      if (chunk == 0 && lse) lse[to] = natural(M, L);
     }
   }
-  p.report(bad);
+  if (bad && a->p.status) atomicOr(a->p.status, bad);
 }
 
 // Joins the pieces of blocks of rows that have several: 32 threads a row, four dimensions each.
 constexpr int kRowsJoined = 8;
 template <int WIDE>
-__global__ __launch_bounds__(32 * kRowsJoined) void paged_rows_join_kernel(Paged p, RowsAttend c) {
+__global__ __launch_bounds__(32 * kRowsJoined) void paged_rows_join_kernel(RowsCall call) {
+  const Paged& p = call.p;
+  const RowsAttend& c = call.c;
   constexpr int kRows = 32 * WIDE;
   const int64_t block_index = blockIdx.x;
   const int parts = c.parts[block_index];
@@ -599,7 +675,7 @@ __global__ __launch_bounds__(32 * kRowsJoined) void paged_rows_join_kernel(Paged
   }
   const int t = (int)(row / c.G);
   const int64_t to = ((c.rows.starts ? c.rows.starts[b] : (int64_t)b * c.rows.rows) + t) * (c.G * p.hkv) + h * c.G + (int)(row - (uint32_t)t * c.G);
-  put_row(c, to, d4, L != 0.f ? y * (1.f / L) : f32x4{0.f, 0.f, 0.f, 0.f});
+  put_row(c.out, c.out_bf16, to, d4, L != 0.f ? y * (1.f / L) : f32x4{0.f, 0.f, 0.f, 0.f});
   if (d4 == 0 && c.lse) c.lse[to] = natural(M, L);
 }
 
