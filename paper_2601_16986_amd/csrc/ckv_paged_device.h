@@ -76,7 +76,10 @@ struct Rows {
   __device__ __forceinline__ RowSpan span(int b, int told, int max_length, int64_t& base) const {
     const int start = starts ? starts[b] : 0, stop = starts ? starts[b + 1] : 0;
     base = starts ? start * row_stride : b * seq_stride;
-    return rows_below(row_span(told, rows, first != nullptr, first ? first[b] : 0, starts != nullptr, start, stop, total), max_length);
+    return span(told, first ? first[b] : 0, start, stop, max_length);
+  }
+  __device__ __forceinline__ RowSpan span(int told, int first_b, int start, int stop, int max_length) const {
+    return rows_below(row_span(told, rows, first != nullptr, first_b, starts != nullptr, start, stop, total), max_length);
   }
 };
 

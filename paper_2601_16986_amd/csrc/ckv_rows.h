@@ -36,23 +36,24 @@ CKV_PLAN u64_t bits_between(long long e0, long long lo, long long hi) {
   return (z >= 64 ? ~0ull : (1ull << z) - 1) & ~((1ull << a) - 1);
 }
 
-// How a call is cut.  Every block of rows has `places` places for pieces of `share` tiles at least.
+// How a call is cut, by what the host knows: every block of rows has `places` places for pieces, of `least` tiles at least.
 struct RowsPlan {
   int wide, blocks;              // wavefronts side by side over rows; blocks of rows per unit (sequence, KV head)
-  int share, places;
+  int least, places, workers;    // workers: compute units
   long long pieces;              // workgroups
 };
 CKV_PLAN RowsPlan rows_plan(long long units, int rows, int group, int entries, int n_cu) {
   const long long all = (long long)rows * group;
-  RowsPlan p = {all <= 32 ? 1 : all <= 64 ? 2 : 4, 0, 0, 1, 0};
+  RowsPlan p = {all <= 32 ? 1 : all <= 64 ? 2 : 4, 0, 0, 1, 0, 0};
   const int each = 32 * p.wide, size = rows_tile(p.wide);
   p.blocks = (int)((all + each - 1) / each);
+  p.least = p.wide == 4 ? 4 : 2;
+  p.workers = n_cu;
   const int tiles = (int)(((long long)entries + size - 1) / size) + 2;          // sinks and window begin inside a tile
-  const long long work = units * p.blocks * tiles, workers = (p.wide == 1 ? 1ll : 2ll) * n_cu;
-  long long share = (work + 2 * workers - 1) / (2 * workers);
-  if (share < 4 * p.wide) share = 4 * p.wide;
-  p.share = share < tiles ? (int)share : tiles;
-  p.places = unit_parts(tiles, p.share);
+  const long long blocks = units * p.blocks, many = (p.wide == 1 ? 2ll : 4ll) * n_cu, most = 1 + (many + blocks - 1) / blocks;
+  p.places = unit_parts(tiles, p.least);
+  if (p.places > most) p.places = (int)most;
+  if (blocks >= many) p.places = 1;
   p.pieces = units * p.blocks * p.places;
   return p;
 }
@@ -62,22 +63,39 @@ CKV_PLAN int rows_share(int tiles, int share, int places) {
   const int least = unit_parts(tiles, places);
   return share > least ? share : least;
 }
+// What a call takes, in the time of a tile that has its compute unit for itself (about 1.1 us): a second workgroup beside it takes the half of that more, except of the one wavefront per SIMD that
+// blocks of 32 rows have room for.  A piece's beginning and end (its rows, pages and first tiles) take as much as 11, joining 4, and what pieces leave for it 3 for 128 rows each.
+struct RowsCost {
+  int block_rows, workers;
+  CKV_PLAN float turn(int k) const { return block_rows > 32 && k > 1 ? 0.75f * k : (float)k; }
+  CKV_PLAN float split(int k, float tiles) const { return turn(k) * (tiles + 11.f) + 4.f + 3.f * k * block_rows / 128; }
+  // whole blocks: the longest, or what each unit has to do and half of that
+  CKV_PLAN float whole(float blocks, float tiles, float longest) const {
+    if (blocks <= workers) return longest + 11.f;
+    if (block_rows > 32 && blocks <= 2 * workers) return 1.5f * (longest + 11.f);
+    return (block_rows > 32 ? 0.75f : 1.f) * (tiles + 11.f * blocks) / workers + 0.5f * longest;
+  }
+};
 
-// Which piece the workgroup `index` takes: workgroups go to the eight parts of the chip in turn, each with a cache of its own, so a unit's pieces go to one of them, units in
-// turn; those of the last units that make no full round are dealt out evenly, neighbours together.  -1: none.
+// Which of all units' `each` blocks of rows the workgroup `index` takes: workgroups go to the eight parts of the chip in turn, each with a cache of its own, so a unit's blocks, which read the
+// same entries, go to one of them, units in turn; those of the last units that make no full round are dealt out evenly, neighbours together.  T(-1): none.  A call's pieces are so many workgroups
+// for all first ones, as many for all second ones and so on: the places that turn out to be empty come last (first to last in each unit they took workgroups' room from what there was to do:
+// 25 rows for 16 sequences in a window of 1024 69 us, not 52).
 constexpr int kParts = 8;
-CKV_PLAN long long rows_grid(long long units, long long each) {
-  const long long full = units / kParts * kParts, rest = (units - full) * each;
+template <class T>
+CKV_PLAN T rows_grid(T units, T each) {
+  const T full = units / kParts * kParts, rest = (units - full) * each;
   return full * each + (rest + kParts - 1) / kParts * kParts;
 }
-CKV_PLAN long long rows_piece(long long index, long long units, long long each) {
-  const long long full = units / kParts * kParts;
+template <class T>
+CKV_PLAN T rows_piece(T index, T units, T each) {
+  const T full = units / kParts * kParts;
   if (index < full * each) {
-    const long long round = index / (kParts * each), in = index - round * kParts * each;
+    const T round = index / (kParts * each), in = index - round * kParts * each;
     return (round * kParts + in % kParts) * each + in / kParts;
   }
-  const long long in = index - full * each, rest = (units - full) * each, chunk = (rest + kParts - 1) / kParts, at = in % kParts * chunk + in / kParts;
-  return at < rest ? full * each + at : -1;
+  const T in = index - full * each, rest = (units - full) * each, chunk = (rest + kParts - 1) / kParts, at = in % kParts * chunk + in / kParts;
+  return at < rest ? full * each + at : T(-1);
 }
 
 }  // namespace ckv

@@ -104,7 +104,7 @@ int ckv_paged_attend_rows(const ckv_pages* pages, const ckv_seqs* seqs, const ck
     return attend_one_row(pages, seqs, &query, queries->first, mask, scale_log2e, out, out_dtype, lse, workspace, workspace_bytes, stream);
   }
   const RowsSplit s = rows_split(pages, seqs, queries->rows, queries->n_q_heads, mask, compute_units());
-  const long long units = (long long)seqs->batch * pages->n_kv_heads, grid = rows_grid(units, (long long)s.plan.blocks * s.plan.places);
+  const long long units = (long long)seqs->batch * pages->n_kv_heads, grid = rows_grid(units, (long long)s.plan.blocks) * s.plan.places;
   if (!launches(grid, kThreads) || !launches(units * s.plan.blocks, 32 * kRowsJoined)) return fail(CKV_EINVAL, "too many rows for one attention (2^24 blocks of 128, a row per query head)");
   if (s.bytes() > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < s.bytes())) return fail(CKV_EWORKSPACE, "workspace too small or misaligned");
   const Paged p = paged_of(pages, seqs);
@@ -122,8 +122,9 @@ int ckv_paged_attend_rows(const ckv_pages* pages, const ckv_seqs* seqs, const ck
   c.sinks = mask->sinks;
   c.out_bf16 = out_dtype == CKV_BF16;
   c.blocks = s.plan.blocks;
-  c.share = s.plan.share;
+  c.least = s.plan.least;
   c.places = s.plan.places;
+  c.workers = s.plan.workers;
   if (s.plan.places > 1) {
     c.partial = (float*)workspace;
     c.ml = (float*)((char*)workspace + s.partial);
@@ -141,7 +142,8 @@ int ckv_paged_attend_rows(const ckv_pages* pages, const ckv_seqs* seqs, const ck
   else attend(std::integral_constant<int, 4>());
   if (int rc = launched("ckv_paged_attend_rows")) return rc;
   if (s.plan.places == 1) return CKV_OK;
-  const dim3 joins((unsigned)(units * s.plan.blocks), (unsigned)(32 * s.plan.wide / kRowsJoined));
+  const long long blocks = units * s.plan.blocks, most = 32 * s.plan.wide / kRowsJoined;
+  const dim3 joins((unsigned)blocks, (unsigned)std::max(1ll, std::min(most, 2048 / blocks)));
   auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, joins, dim3(32 * kRowsJoined), 0, (hipStream_t)stream, RowsCall{p, c}); };
   s.plan.wide == 1 ? join(paged_rows_join_kernel<1>) : s.plan.wide == 2 ? join(paged_rows_join_kernel<2>) : join(paged_rows_join_kernel<4>);
   return launched("ckv_paged_attend_rows");

@@ -26,7 +26,7 @@ struct RowsAttend {
   int64_t units;
   float scale_log2e;
   int32_t G, window, sinks, out_bf16;
-  int32_t blocks, share, places;           // RowsPlan
+  int32_t blocks, least, places, workers;  // RowsPlan
 };
 
 struct RowsCall {
@@ -108,6 +108,57 @@ struct Rest {
   }
 };
 
+// What a sequence's rows are worked out from, asked for with no branch between, so that all of it comes at once.
+struct Told {
+  int length, first, start, stop;
+};
+__device__ __forceinline__ Told told(const Paged& p, const Rows& r, int b) {
+  const int32_t *first = r.first ? r.first : p.lengths, *starts = r.starts ? r.starts : p.lengths;
+  return {p.lengths[b], first[b], starts[b], starts[r.starts ? b + 1 : b]};
+}
+
+// Tiles of a piece, by the lengths as they are: of the ways to have one, two, four or six pieces for each compute unit, and of no pieces, the one that ends first.  Lanes add up their share of
+// the sequences.
+__device__ __forceinline__ int even_share(const Paged& p, const RowsAttend& c, int block_rows, int size, int lane, const Told& mine) {
+  const int per_lane = (p.batch + 63) >> 6, b0 = lane * per_lane;         // mine: sequence b0's
+  struct Have {
+    float blocks, tiles;
+  };
+  auto have = [&](const Told& t) {
+    const RowSpan s = c.rows.span(t.length, t.first, t.start, t.stop, p.max_length);
+    if (s.count == 0) return Have{0.f, 0.f};
+    const int end = s.first + s.count, oldest = c.window ? max(s.first + (c.tree ? 0 : s.count - block_rows / c.G) - c.window, 0) : 0;
+    return Have{(float)(((int64_t)s.count * c.G + block_rows - 1) / block_rows), (float)row_tiles(oldest, end, c.window ? c.sinks : 0, size).count};
+  };
+  Have one = {0.f, 0.f};
+  if (b0 < p.batch) one = have(mine);
+  auto each = [&](auto count) {                    // sum over the sequences' blocks of rows
+    float sum = one.blocks * count(one.tiles);
+    for (int b = b0 + 1; b < b0 + per_lane && b < p.batch; ++b) {
+      const Have more = have(told(p, c.rows, b));
+      sum += more.blocks * count(more.tiles);
+    }
+    return wave_sum_f32(sum) * p.hkv;
+  };
+  float longest = one.tiles;
+  for (int b = b0 + 1; b < b0 + per_lane && b < p.batch; ++b) longest = fmaxf(longest, have(told(p, c.rows, b)).tiles);
+  longest = __uint_as_float(~wave_min_u32(~__float_as_uint(longest)));
+  const float all = each([](float tiles) { return tiles; }), blocks = each([](float) { return 1.f; });
+  const RowsCost cost = {block_rows, c.workers};
+  float best = cost.whole(blocks, all, longest);
+  int share = INT32_MAX;
+#pragma unroll 1
+  for (int k = 1; k <= 6; k += k == 1 ? 1 : 2) {
+    const float most = (float)(k * c.workers);
+    float s = fmaxf(ceilf(all / most), (float)c.least);
+    const float pieces = each([&](float tiles) { return ceilf(tiles / s); });
+    if (pieces > most) s = ceilf(s * pieces / most);
+    const float took = cost.split(k, s);
+    if (took < best) best = took, share = (int)s;
+  }
+  return share;
+}
+
 // One workgroup of four wavefronts per piece: 32 WIDE rows (row = one query head of one of the call's rows of a sequence, heads of a KV head side by side) over some tiles
 // of entries.  A tile's keys and values go through LDS, two tiles in turn, asked for one ahead; 8 bits become bf16 on the way, times their powers of two, which is exact.
 //   logits   K Q^T by 32 x 32 x 16 products, rows = entries, columns = the wavefront's 32 rows, so that a row's maximum and sum are a lane's own but for one exchange of halves;
@@ -128,17 +179,17 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
   __shared__ int s_odd;
   static_assert(sizeof s_tile >= kAttendWaves * 32 * kDim * 4, "the outputs go where the tiles were");
 
-  if (threadIdx.x == 0) s_odd = 0;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i32(tid >> 6), j = lane & 31, half = lane >> 5, wq = wave % WIDE, wk = wave / WIDE;
-  const int64_t each = (int64_t)c.blocks * c.places, piece = rows_piece(blockIdx.x, c.units, each);
-  if (piece < 0) return;
-  const int u = uniform_i32((int)(piece / each)), k_in = uniform_i32((int)(piece - u * each)), part = uniform_i32(k_in / c.blocks), blk = c.blocks - 1 - (k_in - part * c.blocks);      // the last rows have the most to do
-  const int b = uniform_i32(u / p.hkv), h = u - b * p.hkv;
+  if (tid == 0) s_odd = 0;
+  const uint32_t each = (uint32_t)c.blocks, all = rows_grid((uint32_t)c.units, each), part_ = blockIdx.x / all, piece = rows_piece(blockIdx.x - part_ * all, (uint32_t)c.units, each);
+  if (piece == ~0u) return;
+  const int part = uniform_i32((int)part_), u = uniform_i32((int)(piece / each)), blk = uniform_i32((int)(each - 1 - (piece - u * each)));       // the last rows have the most to do
+  const int b = uniform_i32((int)((uint32_t)u / (uint32_t)p.hkv)), h = u - b * p.hkv;
   const int64_t block_index = (int64_t)u * c.blocks + blk;
-  int bad = 0;
-  p.length(b, bad);
-  int64_t q_base;
-  const RowSpan span = c.rows.span(b, uniform_i32(p.lengths[b]), p.max_length, q_base);
+  const Told own = told(p, c.rows, b), mine = told(p, c.rows, min(lane * ((p.batch + 63) >> 6), p.batch - 1));
+  int bad = p.max_length < own.length || own.length < 0 ? PAGED_BAD_LENGTH : 0;
+  const RowSpan span = c.rows.span(uniform_i32(own.length), uniform_i32(own.first), uniform_i32(own.start), uniform_i32(own.stop), p.max_length);
+  const int64_t q_base = c.rows.starts ? uniform_i32(own.start) * c.rows.row_stride : b * c.rows.seq_stride;
   if (span.bad) bad |= PAGED_BAD_LENGTH;
   const uint32_t r0 = (uint32_t)blk * kRows, n_rows = (uint32_t)uniform_i32(span.count) * (uint32_t)c.G;
   if (r0 >= n_rows) {
@@ -153,17 +204,32 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
   const bool valid = row < n_rows;
   const int token = (int)((valid ? row : r0) / c.G), g = (int)((valid ? row : r0) - (uint32_t)token * c.G);
 
+  bf16x8 q[8];                                   // (a block's rows behind the last one: its first once more, and nobody's)
+#pragma unroll
+  for (int s = 0; s < 8; ++s) q[s] = __builtin_bit_cast(bf16x8, load16(c.rows.k + q_base + token * c.rows.row_stride + (h * c.G + g) * c.rows.head_stride + 2 * (16 * s + 8 * half)));
+
   // ---- which entries the lane's row sees: lo .. hi - 1, the first `sinks`, and of the call's rows those in s_see
   const int sinks = c.window ? c.sinks : 0;
   int position = first + token, hi = position + 1, oldest, end = first + t_hi + 1;
   if (c.tree) {
     const int words = (count + 63) >> 6;
-    for (int t = t_lo + wave; t <= t_hi; t += kAttendWaves)
-      for (int w = 0; w < kWords / 2 + 1; ++w) {
-        const int at = 64 * w + lane;
-        const u64 sees = w < words ? __ballot(at < count && c.tree[b * c.tree_seq + t * c.tree_row + at] != 0) : 0ull;
-        if (lane < 2 && 2 * w + lane < kWords) s_see[t - t_lo][2 * w + lane] = (uint32_t)(sees >> 32 * lane);
+    const uint8_t* tree = c.tree + b * c.tree_seq;
+    constexpr int N = 8;                           // rows on their way at once
+    for (int w = 0; w < words; ++w) {
+      const int at = 64 * w + lane;
+      for (int t0 = t_lo + wave; t0 <= t_hi; t0 += N * kAttendWaves) {
+        uint8_t x[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) x[n] = tree[min(t0 + n * kAttendWaves, t_hi) * c.tree_row + min(at, count - 1)];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          const u64 sees = __ballot(at < count && x[n] != 0);
+          if (lane < 2 && t0 + n * kAttendWaves <= t_hi) s_see[t0 + n * kAttendWaves - t_lo][2 * w + lane] = (uint32_t)(sees >> 32 * lane);
+        }
       }
+    }
+    for (int x = tid; x < (t_hi - t_lo + 1) * kWords; x += kThreads)
+      if (x % kWords >= 2 * words) s_see[x / kWords][x % kWords] = 0u;
     __syncthreads();
     auto depth = [&](int t) {
       int n = 0;
@@ -186,18 +252,13 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
 
   RowTiles tiles = row_tiles(oldest, end, sinks, kUnit);
   tiles = {uniform_i32(tiles.sinks), uniform_i32(tiles.base), uniform_i32(tiles.count)};
-  const int share = rows_share(tiles.count, c.share, c.places), parts = unit_parts(tiles.count, share);
+  int share = tiles.count;
+  if (c.places > 1) share = rows_share(tiles.count, even_share(p, c, kRows, kUnit, lane, mine), c.places);
+  const int parts = unit_parts(tiles.count, share);
   if (part == 0 && tid == 0 && c.parts) c.parts[block_index] = parts;
   if (part >= parts) return;
   const int n_first = uniform_i32(part_begin(tiles.count, parts, part)), n_last = uniform_i32(part_begin(tiles.count, parts, part + 1));
 
-  bf16x8 q[8];
-#pragma unroll
-  for (int s = 0; s < 8; ++s) {
-    u32x4 x = {0u, 0u, 0u, 0u};
-    if (valid) x = load16(c.rows.k + q_base + token * c.rows.row_stride + (h * c.G + g) * c.rows.head_stride + 2 * (16 * s + 8 * half));
-    q[s] = __builtin_bit_cast(bf16x8, x);
-  }
   f32x16 acc[4];
   float m_run, l_run;
   const float scale_log2e = c.scale_log2e;
@@ -205,7 +266,7 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
   // ---- units' way into LDS: rows of 256 bytes, bf16 straight there, 8 bits through registers
   const int units = n_last - n_first;
   auto unit_at = [&](int i) CKV_INLINE { return tiles.tile(n_first + i) * kUnit; };
-  auto seen = [&](int e) CKV_INLINE { return e < end && (e >= oldest || e < sinks); };
+  auto seen = [&](int e) CKV_INLINE { return (bool)((e < end) & ((e >= oldest) | (e < sinks))); };
   // Where kPageSlots pages lie, a lane each, of the sequence's pages kPageSlots * window and on, and the ones before them (the pool's first instead of one that is not there).
   struct Known {
     int window = -1;
@@ -214,9 +275,10 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
   u32x4 kr[E4M3 ? NU * kLoads : 1], vr[E4M3 ? NU * kLoads : 1];
   uint32_t ks[E4M3 ? NU * kLoads : 1], vs[E4M3 ? NU * kLoads : 1];
   constexpr int kOnce = E4M3 ? 32 : 16;          // rows of a load
+  constexpr int kMine = kOnce / kAttendWaves;     // of them a wavefront's, always in one page
   const int r_in = tid / (kThreads / kOnce);     // the thread's
   const int shift = p.shift, page_mask = p.page_size() - 1, slot_stride = p.slot_stride;
-  const uint32_t in_row = 16 * (E4M3 ? tid & 7 : (tid & 15) ^ swizzle(r_in)), lane_at = (uint32_t)(r_in * slot_stride) + in_row, next_at = lane_at + (uint32_t)(kOnce * slot_stride);
+  const uint32_t in_row = 16 * (E4M3 ? tid & 7 : (tid & 15) ^ swizzle(r_in)), lane_at = (uint32_t)(r_in * slot_stride) + in_row, next_at = lane_at + (uint32_t)(kOnce * slot_stride), near_at = lane_at - (uint32_t)(kMine * wave * slot_stride);
   const u64 k_to_v = (u64)p.v - (u64)p.k;
   auto pages = [&](int logical, Known& to) CKV_INLINE {
     const auto a = args();
@@ -228,10 +290,6 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
     if (__ballot(needed && !there) != 0ull) s_odd = 1;           // once more, with care
     to.row = (u64)(a->p.k + (there ? page : 0) * a->p.page_stride + h * a->p.head_stride);
     if constexpr (E4M3) to.scale = (u64)(a->p.scales + (there ? page : 0) * a->p.scale_page_stride + h * a->p.scale_head_stride);
-  };
-  auto of_slot = [&](u64 v, int slot) CKV_INLINE {
-    const uint32_t x = (uint32_t)__builtin_amdgcn_ds_bpermute(slot << 2, (int)(uint32_t)v), z = (uint32_t)__builtin_amdgcn_ds_bpermute(slot << 2, (int)(uint32_t)(v >> 32));
-    return (u64)z << 32 | x;
   };
   const uint32_t k_lds = lds_at(&s_tile[0][0][0]), v_lds = lds_at(&s_tile[1][0][0]);
 
@@ -303,15 +361,17 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
         }
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-          const int e = e0 + kOnce * i + r_in, slot = (e >> shift) & (kPageSlots - 1), off = e & page_mask;
-          const u64 row = of_slot(from.row, slot) + (side ? k_to_v : 0ull) + (uint32_t)(off * slot_stride) + in_row;
+          const int e = e0 + kOnce * i + kMine * wave, slot = (e >> shift) & (kPageSlots - 1), off = e & page_mask;
+          const u64 row = readlane_u64(from.row, slot) + (side ? k_to_v : 0ull) + (uint32_t)(off * slot_stride);
+          const bool nobody = side && !((bool)((unit >= 0) & (unit < units)) & seen(e + r_in - kMine * wave));
           if constexpr (E4M3) {
-            at[side][s * kLoads + i] = row;
-            scale_of[side][s * kLoads + i] = of_slot(from.scale, slot) + (uint32_t)(2 * off + side);
-            if (side && !(unit >= 0 && unit < units && seen(e))) unseen |= 1u << (s * kLoads + i);
+            at[side][s * kLoads + i] = row + near_at;
+            scale_of[side][s * kLoads + i] = readlane_u64(from.scale, slot) + (uint32_t)(2 * (off + r_in - kMine * wave) + side);
+            if (nobody) unseen |= 1u << (s * kLoads + i);
           } else {
             const uint32_t to = (side ? v_lds : k_lds) + buf * kBuf + s * kUnit * 256 + (16 * i + 4 * wave) * 256;
-            load_to_lds(!side || (unit >= 0 && unit < units && seen(e)) ? (const uint8_t*)row : kNothing + 16 * (tid & 15), to);
+            if (side) load_to_lds(nobody ? kNothing + 16 * (tid & 15) : (const uint8_t*)row + near_at, to);
+            else load_to_lds((const uint8_t*)row, near_at, to);
           }
         }
       }
@@ -617,36 +677,49 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
   const auto a = args();
   const int G = a->c.G, hkv = a->p.hkv;
   const int64_t out_row = a->c.rows.starts ? a->c.rows.starts[b] : (int64_t)b * a->c.rows.rows;
-  float* lse = a->c.lse;
-  for (int x = tid; x < kRows * (kDim / 4); x += kThreads) {
-    const int r = x >> 5, chunk = x & 31, in = r & 31;
-    if (r0 + r >= n_rows) break;
-    float M = kNoLogit, L = 0.f;
+  float *lse = a->c.lse, *partial = a->c.partial, *ml = a->c.ml;
+  uint8_t* out = a->c.out;
+  const bool out_bf16 = a->c.out_bf16;
+  const int places = a->c.places;
+  constexpr int kEnd = 4;                          // rows at once
+  const int chunk = tid & 31;
+  for (int r_first = tid >> 5; r_first < kRows; r_first += kThreads / 32 * kEnd) {
+    f32x4 y[kEnd];
+    float M[kEnd], L[kEnd];
 #pragma unroll
-    for (int k = 0; k < kDeep; ++k) M = fmaxf(M, s_m[k * WIDE + (r >> 5)][in]);
-    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < kEnd; ++i) {
+      const int r = r_first + kThreads / 32 * i, in = r & 31;
+      M[i] = kNoLogit, L[i] = 0.f, y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < kDeep; ++k) {
-      const int w = k * WIDE + (r >> 5);
-      const float f = fast_exp2(s_m[w][in] - M);
-      L += s_l[w][in] * f;
-      y += *reinterpret_cast<const f32x4*>(s_o + (w * 32 + in) * kDim + 4 * (chunk ^ in)) * f;
+      for (int k = 0; k < kDeep; ++k) M[i] = fmaxf(M[i], s_m[k * WIDE + (r >> 5)][in]);
+#pragma unroll
+      for (int k = 0; k < kDeep; ++k) {
+        const int w = k * WIDE + (r >> 5);
+        const float f = fast_exp2(s_m[w][in] - M[i]);
+        L[i] += s_l[w][in] * f;
+        y[i] += *reinterpret_cast<const f32x4*>(s_o + (w * 32 + in) * kDim + 4 * (chunk ^ in)) * f;
+      }
     }
-    if (parts > 1) {
-      const int64_t at = (block_index * a->c.places + part) * kRows + r;
-      *reinterpret_cast<f32x4*>(a->c.partial + at * kDim + 4 * chunk) = y;
-      if (chunk == 0) a->c.ml[2 * at] = M, a->c.ml[2 * at + 1] = L;
-    } else {
-      const int t = (int)((r0 + r) / G);
-      const int64_t to = (out_row + t) * (G * hkv) + h * G + (int)(r0 + r - (uint32_t)t * G);
-      put_row(a->c.out, a->c.out_bf16, to, 4 * chunk, L != 0.f ? y * (1.f / L) : f32x4{0.f, 0.f, 0.f, 0.f});
-      if (chunk == 0 && lse) lse[to] = natural(M, L);
+#pragma unroll
+    for (int i = 0; i < kEnd; ++i) {
+      const int r = r_first + kThreads / 32 * i;
+      if (r0 + r >= n_rows) break;
+      if (parts > 1) {
+        const int64_t at = (block_index * places + part) * kRows + r;
+        *reinterpret_cast<f32x4*>(partial + at * kDim + 4 * chunk) = y[i];
+        if (chunk == 0) *reinterpret_cast<f32x2*>(ml + 2 * at) = f32x2{M[i], L[i]};
+      } else {
+        const int t = (int)((r0 + r) / G);
+        const int64_t to = (out_row + t) * (G * hkv) + h * G + (int)(r0 + r - (uint32_t)t * G);
+        put_row(out, out_bf16, to, 4 * chunk, L[i] != 0.f ? y[i] * (1.f / L[i]) : f32x4{0.f, 0.f, 0.f, 0.f});
+        if (chunk == 0 && lse) lse[to] = natural(M[i], L[i]);
+      }
     }
   }
   if (bad && a->p.status) atomicOr(a->p.status, bad);
 }
 
-// Joins the pieces of blocks of rows that have several: 32 threads a row, four dimensions each.
+// Joins the pieces of blocks of rows that have several: 32 threads a row, four dimensions each, eight rows a workgroup, which takes every `gridDim.y`-th eight of a block.
 constexpr int kRowsJoined = 8;
 template <int WIDE>
 __global__ __launch_bounds__(32 * kRowsJoined) void paged_rows_join_kernel(RowsCall call) {
@@ -659,24 +732,41 @@ __global__ __launch_bounds__(32 * kRowsJoined) void paged_rows_join_kernel(RowsC
   const int u = (int)(block_index / c.blocks), blk = (int)(block_index - (int64_t)u * c.blocks), b = u / p.hkv, h = u - b * p.hkv;
   int64_t base;
   const RowSpan span = c.rows.span(b, p.lengths[b], p.max_length, base);
-  const int in = blockIdx.y * kRowsJoined + (threadIdx.x >> 5), d4 = 4 * (threadIdx.x & 31);
-  const uint32_t row = (uint32_t)blk * kRows + in;
-  if (row >= (uint32_t)span.count * (uint32_t)c.G) return;
-  float M = kNoLogit, L = 0.f;
-  f32x4 y = {0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < parts; ++i) {
-    const int64_t at = (block_index * c.places + i) * kRows + in;
-    const f32x2 st = *reinterpret_cast<const f32x2*>(c.ml + 2 * at);
-    const f32x4 x = *reinterpret_cast<const f32x4*>(c.partial + at * kDim + d4);
-    const float m = fmaxf(M, st[0]), old = fast_exp2(M - m), now = fast_exp2(st[0] - m);
-    M = m;
-    L = L * old + st[1] * now;
-    y = y * old + x * now;
+  const int d4 = 4 * (threadIdx.x & 31);
+  for (int in = blockIdx.y * kRowsJoined + (threadIdx.x >> 5); in < kRows; in += kRowsJoined * gridDim.y) {
+    const uint32_t row = (uint32_t)blk * kRows + in;
+    if (row >= (uint32_t)span.count * (uint32_t)c.G) return;
+    float M = kNoLogit, L = 0.f;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    constexpr int N = 8;                           // parts on their way at once
+    for (int i0 = 0; i0 < parts; i0 += N) {
+      f32x2 st[N];
+      f32x4 x[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int64_t at = (block_index * c.places + min(i0 + i, parts - 1)) * kRows + in;
+        st[i] = *reinterpret_cast<const f32x2*>(c.ml + 2 * at);
+        x[i] = *reinterpret_cast<const f32x4*>(c.partial + at * kDim + d4);
+      }
+      float m = M;
+#pragma unroll
+      for (int i = 0; i < N; ++i) m = fmaxf(m, st[i][0]);
+      const float old = fast_exp2(M - m);
+      M = m;
+      L *= old;
+      y = y * old;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float now = i0 + i < parts ? fast_exp2(st[i][0] - m) : 0.f;
+        L += st[i][1] * now;
+        y += x[i] * now;
+      }
+    }
+    const int t = (int)(row / c.G);
+    const int64_t to = ((c.rows.starts ? c.rows.starts[b] : (int64_t)b * c.rows.rows) + t) * (c.G * p.hkv) + h * c.G + (int)(row - (uint32_t)t * c.G);
+    put_row(c.out, c.out_bf16, to, d4, L != 0.f ? y * (1.f / L) : f32x4{0.f, 0.f, 0.f, 0.f});
+    if (d4 == 0 && c.lse) c.lse[to] = natural(M, L);
   }
-  const int t = (int)(row / c.G);
-  const int64_t to = ((c.rows.starts ? c.rows.starts[b] : (int64_t)b * c.rows.rows) + t) * (c.G * p.hkv) + h * c.G + (int)(row - (uint32_t)t * c.G);
-  put_row(c.out, c.out_bf16, to, d4, L != 0.f ? y * (1.f / L) : f32x4{0.f, 0.f, 0.f, 0.f});
-  if (d4 == 0 && c.lse) c.lse[to] = natural(M, L);
 }
 
 }  // namespace ckv
