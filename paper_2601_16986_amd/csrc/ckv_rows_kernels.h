@@ -88,6 +88,9 @@ __device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t lane_a
   base = uniform_at(base);
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(lane_at), "s"(base) : "memory");
 }
+// What lies `more` bytes behind `base`, which is global memory: taken for any memory its load would be waited for as reads of LDS are, by those that follow.
+template <class T>
+__device__ __forceinline__ T global_at(u64 base, uint32_t more) { return *(const __attribute__((address_space(1))) T*)(base + more); }
 __device__ __forceinline__ void arrived() { __builtin_amdgcn_s_waitcnt(0x0F70); }          // vmcnt(0)
 
 __device__ __forceinline__ u32x4 read_row(uint32_t at, int more) { return *(const __attribute__((address_space(3))) u32x4*)((const lds8*)(uintptr_t)at + more); }
@@ -254,7 +257,7 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
   tiles = {uniform_i32(tiles.sinks), uniform_i32(tiles.base), uniform_i32(tiles.count)};
   int share = tiles.count;
   if (c.places > 1) share = rows_share(tiles.count, even_share(p, c, kRows, kUnit, lane, mine), c.places);
-  const int parts = unit_parts(tiles.count, share);
+  const int parts = uniform_i32(unit_parts(tiles.count, share));
   if (part == 0 && tid == 0 && c.parts) c.parts[block_index] = parts;
   if (part >= parts) return;
   const int n_first = uniform_i32(part_begin(tiles.count, parts, part)), n_last = uniform_i32(part_begin(tiles.count, parts, part + 1));
@@ -278,7 +281,8 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
   constexpr int kMine = kOnce / kAttendWaves;     // of them a wavefront's, always in one page
   const int r_in = tid / (kThreads / kOnce);     // the thread's
   const int shift = p.shift, page_mask = p.page_size() - 1, slot_stride = p.slot_stride;
-  const uint32_t in_row = 16 * (E4M3 ? tid & 7 : (tid & 15) ^ swizzle(r_in)), lane_at = (uint32_t)(r_in * slot_stride) + in_row, next_at = lane_at + (uint32_t)(kOnce * slot_stride), near_at = lane_at - (uint32_t)(kMine * wave * slot_stride);
+  const uint32_t in_row = 16 * (E4M3 ? tid & 7 : (tid & 15) ^ swizzle(r_in)), lane_at = (uint32_t)(r_in * slot_stride) + in_row, next_at = lane_at + (uint32_t)(kOnce * slot_stride), wave_at = (uint32_t)(kMine * wave * slot_stride), near_at = lane_at - wave_at;
+  const uint32_t scale_near = (uint32_t)(2 * (r_in - kMine * wave));
   const u64 k_to_v = (u64)p.v - (u64)p.k;
   auto pages = [&](int logical, Known& to) CKV_INLINE {
     const auto a = args();
@@ -300,7 +304,8 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
     u64 k_row[NU], k_scale[NU];
   } last = {}, last2 = {};         // of the units whose keys were asked for last, and before that
   uint32_t unseen = 0u;
-  // 8 bits go into registers, with no branch around their loads: loaded registers would be copied where ways meet, and waited for.  So the ways only work out places.
+  // 8 bits go into registers, with no branch around their loads: loaded registers would be copied where ways meet, and waited for.  So the ways only work out places (the wavefront's; a lane's is so
+  // much further on in all of them).
   u64 at[E4M3 ? 2 : 1][E4M3 ? NU * kLoads : 1], scale_of[E4M3 ? 2 : 1][E4M3 ? NU * kLoads : 1];
   auto ask_easy = [&](int n, int buf) CKV_INLINE {
     Rows4 now;
@@ -318,12 +323,13 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
           if constexpr (E4M3) {
-            at[side][s * kLoads + i] = row + (i & 1 ? next_at : lane_at);
-            scale_of[side][s * kLoads + i] = scale + (uint32_t)(2 * (kOnce * i + r_in));
+            at[side][s * kLoads + i] = row + wave_at;
+            scale_of[side][s * kLoads + i] = scale + (uint32_t)(2 * (kOnce * i + kMine * wave));
           } else {
             load_to_lds((const uint8_t*)row, i & 1 ? next_at : lane_at, (side ? v_lds : k_lds) + buf * kBuf + s * kUnit * 256 + (16 * i + 4 * wave) * 256);
           }
-          if (i & 1) row += (uint32_t)(2 * kOnce * slot_stride);
+          if constexpr (E4M3) row += (uint32_t)(kOnce * slot_stride);
+          else if (i & 1) row += (uint32_t)(2 * kOnce * slot_stride);
         }
       }
     }
@@ -349,9 +355,9 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
             pages(w * kPageSlots + lane, known);
           }
           from = known;
-          if (!all) plain = unit + 1;
+          if (!all) plain = uniform_i32(unit + 1);
           const int left = min((w + 1) * kPageSlots << shift, end) - e0, slot = (e0 >> shift) & (kPageSlots - 1), off = e0 & page_mask;
-          easy = all && page_mask + 1 >= kUnit && n_first + unit >= tiles.sinks ? min(units, unit + left / kUnit) : 0;
+          easy = all && page_mask + 1 >= kUnit && n_first + unit >= tiles.sinks ? uniform_i32(min(units, unit + left / kUnit)) : 0;
           last.k_row[s] = readlane_u64(known.row, slot) + (uint32_t)(off * slot_stride);
           if constexpr (E4M3) last.k_scale[s] = readlane_u64(known.scale, slot) + (uint32_t)(2 * off);
         } else {
@@ -365,8 +371,8 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
           const u64 row = readlane_u64(from.row, slot) + (side ? k_to_v : 0ull) + (uint32_t)(off * slot_stride);
           const bool nobody = side && !((bool)((unit >= 0) & (unit < units)) & seen(e + r_in - kMine * wave));
           if constexpr (E4M3) {
-            at[side][s * kLoads + i] = row + near_at;
-            scale_of[side][s * kLoads + i] = readlane_u64(from.scale, slot) + (uint32_t)(2 * (off + r_in - kMine * wave) + side);
+            at[side][s * kLoads + i] = row;
+            scale_of[side][s * kLoads + i] = readlane_u64(from.scale, slot) + (uint32_t)(2 * off + side);
             if (nobody) unseen |= 1u << (s * kLoads + i);
           } else {
             const uint32_t to = (side ? v_lds : k_lds) + buf * kBuf + s * kUnit * 256 + (16 * i + 4 * wave) * 256;
@@ -383,10 +389,10 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
     if constexpr (E4M3) {
 #pragma unroll
       for (int i = 0; i < NU * kLoads; ++i) {
-        kr[i] = load16((const uint8_t*)at[0][i]);
-        ks[i] = *(const uint8_t*)scale_of[0][i];
-        vr[i] = load16((const uint8_t*)at[1][i]);
-        vs[i] = *(const uint8_t*)scale_of[1][i];
+        kr[i] = global_at<u32x4>(at[0][i], near_at);
+        ks[i] = global_at<uint8_t>(scale_of[0][i], scale_near);
+        vr[i] = global_at<u32x4>(at[1][i], near_at);
+        vs[i] = global_at<uint8_t>(scale_of[1][i], scale_near);
       }
     }
   };
