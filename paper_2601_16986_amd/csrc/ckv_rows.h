@@ -8,6 +8,14 @@ typedef unsigned long long u64_t;
 
 constexpr int kMaxDrafts = 512;        // rows of a sequence in a call with a tree
 
+// Workgroups that share the heads of a page's rows where rows enter with their rotation, of `pages` that rows may reach: as many as find a compute unit of their own, where there are more rows
+// than a workgroup turns at once and so many heads (key and value are one).
+CKV_PLAN int turned_by(long long pages, int rows, int group, int n_cu) {
+  if (rows <= 16 || pages <= 0) return 1;
+  const long long many = n_cu / pages;
+  return many < 1 ? 1 : many < group + 1 ? (int)many : group + 1;
+}
+
 // A workgroup of four wavefronts has 32, 64 or 128 rows (a row is a query head of one of the call's rows), which its wavefronts share, 32 each; where fewer wavefronts do, each of
 // them has its part of the entries.  `wide`: wavefronts side by side over rows, 1, 2 or 4.
 // The entries that they take at once, 32 each, are a tile.

@@ -182,7 +182,8 @@ int ckv_paged_append_rotated(const ckv_pages* pages, const ckv_seqs* seqs, const
   c.magnitude = rotation->magnitude;
   c.pairs = rotation->n_pairs;
   c.interleaved = rotation->interleaved;
-  const dim3 grid((unsigned)(seqs->batch * pages->n_kv_heads), touched);
+  const long long units = (long long)seqs->batch * pages->n_kv_heads;
+  const dim3 grid((unsigned)units, touched, (unsigned)turned_by(units * touched, rows->rows, c.G, compute_units()));
   auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, (hipStream_t)stream, p, r, c); };
   pages->dtype == CKV_E4M3 ? launch(paged_append_rotated_kernel<true>) : launch(paged_append_rotated_kernel<false>);
   return launched("ckv_paged_append_rotated");
