@@ -425,17 +425,18 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
   uint32_t k_at_ = k_lds + (wk * 32 + j) * 256 + ((half ^ swizzle(j)) << 4);
   const int l16 = lane & 15;
   uint32_t v_at_ = v_lds + (wk * 32 + 4 * half + (l16 >> 2)) * 256 + ((l16 >> 2) << 6 | ((((lane >> 4) & 1) * 2 + ((l16 >> 1) & 1)) ^ half) << 4 | (l16 & 1) * 8);
-  // (With registers that 8 bits need on their way these places are worked out again and again, not kept.)
-  auto keys = [&](int x, int at) CKV_INLINE {
-    uint32_t k_at = k_at_;
-    if constexpr (E4M3) here(k_at);
-    return read_row(k_at ^ 32 * x, at);
+  // (With registers that 8 bits need on their way these places are worked out again and again, not kept, each in one instruction.)
+  auto otherwise = [](uint32_t at, int bits) CKV_INLINE {
+    if constexpr (!E4M3) return at ^ bits;
+    if (bits == 0) return at;
+    uint32_t y;
+    asm volatile("v_xor_b32 %0, %1, %2" : "=v"(y) : "i"(bits), "v"(at));
+    return y;
   };
+  auto keys = [&](int x, int at) CKV_INLINE { return read_row(otherwise(k_at_, 32 * x), at); };
   auto values = [&](int n, int at, s16x4 (&v)[2]) CKV_INLINE {                       // n = 2 d + x: dimensions 32 d and on, entries 16 x and on
-    uint32_t v_at = v_at_;
-    if constexpr (E4M3) here(v_at);
-    v[0] = read_transposed(v_at ^ 64 * (n >> 1), at + (n & 1) * 16 * 256);
-    v[1] = read_transposed(v_at ^ (64 * (n >> 1) + 32), at + (n & 1) * 16 * 256 + 8 * 256);
+    v[0] = read_transposed(otherwise(v_at_, 64 * (n >> 1)), at + (n & 1) * 16 * 256);
+    v[1] = read_transposed(otherwise(v_at_, 64 * (n >> 1) + 32), at + (n & 1) * 16 * 256 + 8 * 256);
   };
   auto product = [](s16x8 a, u32x4 w, f32x16 c) CKV_INLINE { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, w), c, 0, 0, 0); };
   auto logits = [&](u32x4 k, int x, f32x16 c) CKV_INLINE { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), q[x], c, 0, 0, 0); };
