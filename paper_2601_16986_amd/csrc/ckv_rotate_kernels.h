@@ -136,10 +136,11 @@ struct Pairing {
 // One workgroup per (sequence, KV head with its queries) and page that new rows reach, as in paged_append_kernel.  Sixteen lanes take a row: each works out the sines and
 // cosines of four pairs and gives them to those who need them, then the row's heads go by, key and value first, kAhead of them on their way at once; where the page gets
 // fewer than sixteen rows, sixteen lanes take some of a row's heads.  Where pages are few, more workgroups (blockIdx.z) share a page's heads, the first of them keys and values too
-// (turned_by; 64 rows of 4 sequences with 8 heads for each of 4 KV heads: 13.3 us by one, 9.4 by eight).
+// (SHARED, turned_by; 64 rows of 4 sequences with 8 heads for each of 4 KV heads: 13.3 us by one, 9.4 by eight).
 constexpr int kTurnAhead = 4;
-template <bool E4M3>
+template <bool E4M3, bool SHARED>
 __global__ __launch_bounds__(kThreads) void paged_append_rotated_kernel(Paged p, Rows r, Turned c) {
+  const int z = SHARED ? blockIdx.z : 0;
   constexpr int kGroups = kThreads / 16;
   __shared__ float s_lo[kThreads / 64][kDim], s_hi[kThreads / 64][kDim];
   const int u = blockIdx.x, b = u / p.hkv, h = u - b * p.hkv;
@@ -152,11 +153,11 @@ __global__ __launch_bounds__(kThreads) void paged_append_rotated_kernel(Paged p,
   const int col = (span.first >> p.shift) + blockIdx.y;
   const int begin = max(span.first, col << p.shift), end = (int)min((int64_t)span.first + span.count, ((int64_t)col + 1) << p.shift);
   if (begin >= end || col >= p.columns) {
-    if (blockIdx.y == 0 && blockIdx.z == 0 && tid == 0) p.report(bad);
+    if (blockIdx.y == 0 && z == 0 && tid == 0) p.report(bad);
     return;
   }
   const int page = p.page(b, col, bad);
-  if (blockIdx.z == 0 && tid == 0) p.report(bad);
+  if (z == 0 && tid == 0) p.report(bad);
   const int64_t at = (int64_t)page * p.page_stride + h * p.head_stride;
   const int64_t start = r.starts ? r.starts[b] : 0;
   const uint8_t* q0 = c.q + (r.starts ? start * c.q_row : b * c.q_seq) + (int64_t)h * c.G * c.q_head + 16 * piece;
@@ -171,7 +172,7 @@ __global__ __launch_bounds__(kThreads) void paged_append_rotated_kernel(Paged p,
   int parts = 1;                                       // of a row's heads
   while (parts < kGroups && 2 * parts * (end - begin) <= kGroups) parts *= 2;
   const int part = group & (parts - 1), heads = c.G + 1, rows_each = kGroups / parts;       // the key and value, then the queries
-  const int first_head = part + parts * blockIdx.z, every = parts * gridDim.z;
+  const int first_head = part + parts * z, every = SHARED ? parts * gridDim.z : parts;
   Extremes<E4M3, kThreads> extremes;
   for (int row = begin + group / parts; row < end; row += rows_each) {
     const int i = row - span.first, slot = row & (p.page_size() - 1), position = positions ? positions[i] : row;
@@ -228,7 +229,7 @@ __global__ __launch_bounds__(kThreads) void paged_append_rotated_kernel(Paged p,
       }
     }
   }
-  if (p.bounds && page >= 0 && blockIdx.z == 0) extremes.write(p, page, h, col, begin, end, length, s_lo, s_hi, tid);
+  if (p.bounds && page >= 0 && z == 0) extremes.write(p, page, h, col, begin, end, length, s_lo, s_hi, tid);
 }
 
 }  // namespace ckv

@@ -185,7 +185,8 @@ int ckv_paged_append_rotated(const ckv_pages* pages, const ckv_seqs* seqs, const
   const long long units = (long long)seqs->batch * pages->n_kv_heads;
   const dim3 grid((unsigned)units, touched, (unsigned)turned_by(units * touched, rows->rows, c.G, compute_units()));
   auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, (hipStream_t)stream, p, r, c); };
-  pages->dtype == CKV_E4M3 ? launch(paged_append_rotated_kernel<true>) : launch(paged_append_rotated_kernel<false>);
+  if (grid.z > 1) pages->dtype == CKV_E4M3 ? launch(paged_append_rotated_kernel<true, true>) : launch(paged_append_rotated_kernel<false, true>);
+  else pages->dtype == CKV_E4M3 ? launch(paged_append_rotated_kernel<true, false>) : launch(paged_append_rotated_kernel<false, false>);
   return launched("ckv_paged_append_rotated");
 }
 
