@@ -31,7 +31,7 @@ CKV_PLAN RowTiles row_tiles(int oldest, int end, int sinks, int size) {
   if (end <= 0) return {0, 0, 0};
   if (oldest > end) oldest = end;
   const int few = sinks < oldest ? sinks : oldest;                      // sinks that lie before the window
-  int head = (few + size - 1) / size, base = oldest / size;
+  int head = few / size + (few % size != 0), base = oldest / size;
   const int last = (int)(((long long)end + size - 1) / size);
   if (base < head) base = head;
   return {head, base, head + (last > base ? last - base : 0)};

@@ -70,6 +70,20 @@ def test_rows_in_few_and_many_pieces(batch, length, hkv, rows, g):
     check_rows(f, q, out, counts, lse=lse, only=[b for b in range(batch) if b < 2 or b % 41 == 0])
 
 
+@pytest.mark.parametrize("batch,length,rows,g,window", [(100, 5000, 4, 4, 0), (70, 3099, 40, 4, 0), (129, 2500, 15, 4, 700)])
+def test_pieces_by_the_lengths_of_more_sequences_than_a_wavefront_has_lanes(batch, length, rows, g, window):
+    rng = np.random.default_rng(batch)
+    lengths = [length, 0] + [int(x) for x in np.exp(rng.uniform(0, np.log(length), batch - 2))]
+    counts = [min(n, rows) for n in lengths]
+    f = Filled(lengths, 1, 64, True, seed=batch)
+    q = queries(f, rows, g)
+    out, lse = attend(f, q, counts, lse=True, f32=True, window=window)
+    check_rows(f, q, out, counts, window=window, lse=lse, only=[b for b in range(batch) if b < 2 or b % 23 == 0])
+    packed = torch.cat([device(q)[b, :n] for b, n in enumerate(counts)])
+    again, _ = f.cache.attend_rows(f.seqs, packed, rows=rows, starts=ints(np.cumsum([0] + counts)), f32=True, window=window)
+    assert torch.equal(again, torch.cat([out[b, :n] for b, n in enumerate(counts)]))
+
+
 def test_peaked_and_large_logits():
     f = Filled([300, 77], 2, 16, True, seed=9, spread=3.0)
     q = queries(f, 20, 8, spread=3.0)
