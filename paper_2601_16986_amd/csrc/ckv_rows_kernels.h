@@ -295,7 +295,7 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
     to.row = (u64)(a->p.k + (there ? page : 0) * a->p.page_stride + h * a->p.head_stride);
     if constexpr (E4M3) to.scale = (u64)(a->p.scales + (there ? page : 0) * a->p.scale_page_stride + h * a->p.scale_head_stride);
   };
-  const uint32_t k_lds = lds_at(&s_tile[0][0][0]), v_lds = lds_at(&s_tile[1][0][0]);
+  const uint32_t k_lds = lds_at(&s_tile[0][0][0]), v_lds = k_lds + 2 * kBuf;
 
   // The n-th buffers take keys of units NU n + 1 and on, values of units NU n - 1 and on.  The easy way, while units' entries follow one another, each unit in one page of those that are known, all of
   // them seen by some row: a page's place out of its lane, and values where the keys of two units before were.  Units below `easy`, from `plain` on (values), may go it.
