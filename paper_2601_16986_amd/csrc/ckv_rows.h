@@ -16,9 +16,9 @@ CKV_PLAN int turned_by(long long pages, int rows, int group, int n_cu) {
   return many < 1 ? 1 : many < group + 1 ? (int)many : group + 1;
 }
 
-// A workgroup of four wavefronts has 32, 64 or 128 rows (a row is a query head of one of the call's rows), which its wavefronts share, 32 each; where fewer wavefronts do, each of
-// them has its part of the entries.  `wide`: wavefronts side by side over rows, 1, 2 or 4.
-// The entries that they take at once, 32 each, are a tile.
+// A workgroup of four wavefronts has 64 or 128 rows (a row is a query head of one of the call's rows), 32 for each of `wide` = 2 or 4 wavefronts side by side; where two do, the others have the other
+// half of the entries.  The entries that they take at once, 32 each, are a tile.  128 rows where there are more than 64: what goes through LDS serves twice as many (us in blocks of 64 and of 128, over 4096 entries
+// of 32 sequences with 8 KV heads, then 777 of 4 with 4: 128 rows 163 and 152, 23.4 and 24.4; 64 rows 106 and 121, 19.7 and 22.2; 32 rows 83 and 101, 18.3 and 21.5).
 CKV_PLAN int rows_tile(int wide) { return 128 / wide; }
 
 // Which entries a block of rows has to look at, in tiles: those of the first `sinks` entries, and those from the oldest that any row's window holds up to the end of the
@@ -44,7 +44,9 @@ CKV_PLAN u64_t bits_between(long long e0, long long lo, long long hi) {
   return (z >= 64 ? ~0ull : (1ull << z) - 1) & ~((1ull << a) - 1);
 }
 
-// How a call is cut, by what the host knows: every block of rows has `places` places for pieces, of `least` tiles at least.
+// How a call is cut, by what the host knows: every block of rows has `places` places for pieces, of `least` tiles at least (us with 1, 2, 3, 4, 6 tiles of 64 rows, 13 in all: 17.9, 18.5, 20.3, 21.9, -;
+// of 128 rows, 25 in all: -, 23.4, 22.3, 23.8, 24.0).  Up to four pieces for each compute unit, none where there are as many blocks: a piece beside whole blocks costs its beginning, end and joining for nothing
+// (384 blocks of one length 217 us whole, 234 in pieces), but sequences of many lengths leave units idle without (64 drafts of 32 of them 389 whole, 358 in pieces; one sequence of 131072 4360 and 254).
 struct RowsPlan {
   int wide, blocks;              // wavefronts side by side over rows; blocks of rows per unit (sequence, KV head)
   int least, places, workers;    // workers: compute units
@@ -52,13 +54,13 @@ struct RowsPlan {
 };
 CKV_PLAN RowsPlan rows_plan(long long units, int rows, int group, int entries, int n_cu) {
   const long long all = (long long)rows * group;
-  RowsPlan p = {all <= 32 ? 1 : all <= 64 ? 2 : 4, 0, 0, 1, 0, 0};
+  RowsPlan p = {all <= 64 ? 2 : 4, 0, 0, 1, 0, 0};
   const int each = 32 * p.wide, size = rows_tile(p.wide);
   p.blocks = (int)((all + each - 1) / each);
-  p.least = p.wide == 4 ? 4 : 2;
+  p.least = p.wide == 4 ? 3 : 1;
   p.workers = n_cu;
   const int tiles = (int)(((long long)entries + size - 1) / size) + 2;          // sinks and window begin inside a tile
-  const long long blocks = units * p.blocks, many = (p.wide == 1 ? 2ll : 4ll) * n_cu, most = 1 + (many + blocks - 1) / blocks;
+  const long long blocks = units * p.blocks, many = 4ll * n_cu, most = 1 + (many + blocks - 1) / blocks;
   p.places = unit_parts(tiles, p.least);
   if (p.places > most) p.places = (int)most;
   if (blocks >= many) p.places = 1;
@@ -71,17 +73,17 @@ CKV_PLAN int rows_share(int tiles, int share, int places) {
   const int least = unit_parts(tiles, places);
   return share > least ? share : least;
 }
-// What a call takes, in the time of a tile that has its compute unit for itself (about 1.1 us): a second workgroup beside it takes the half of that more, except of the one wavefront per SIMD that
-// blocks of 32 rows have room for.  A piece's beginning and end (its rows, pages and first tiles) take as much as 11, joining 4, and what pieces leave for it 3 for 128 rows each.
+// What a call takes, in the time of a tile that has its compute unit for itself (about 1.1 us): two side by side take half as
+// long again.  A piece's beginning and end (its rows, pages and first tiles) take as much as 11, joining 4, and what pieces leave for it 3 for 128 rows each.
 struct RowsCost {
   int block_rows, workers;
-  CKV_PLAN float turn(int k) const { return block_rows > 32 && k > 1 ? 0.75f * k : (float)k; }
+  CKV_PLAN float turn(int k) const { return k > 1 ? 0.75f * k : 1.f; }
   CKV_PLAN float split(int k, float tiles) const { return turn(k) * (tiles + 11.f) + 4.f + 3.f * k * block_rows / 128; }
   // whole blocks: the longest, or what each unit has to do and half of that
   CKV_PLAN float whole(float blocks, float tiles, float longest) const {
     if (blocks <= workers) return longest + 11.f;
-    if (block_rows > 32 && blocks <= 2 * workers) return 1.5f * (longest + 11.f);
-    return (block_rows > 32 ? 0.75f : 1.f) * (tiles + 11.f * blocks) / workers + 0.5f * longest;
+    if (blocks <= 2 * workers) return 1.5f * (longest + 11.f);
+    return 0.75f * (tiles + 11.f * blocks) / workers + 0.5f * longest;
   }
 };
 

@@ -137,15 +137,13 @@ int ckv_paged_attend_rows(const ckv_pages* pages, const ckv_seqs* seqs, const ck
     c.out_bf16 ? launch(paged_rows_kernel<E4M3, WIDE, 2>) : launch(paged_rows_kernel<E4M3, WIDE, 3>);
   };
   auto attend = [&](auto wide) { pages->dtype == CKV_E4M3 ? terms(std::true_type(), wide) : terms(std::false_type(), wide); };
-  if (s.plan.wide == 1) attend(std::integral_constant<int, 1>());
-  else if (s.plan.wide == 2) attend(std::integral_constant<int, 2>());
-  else attend(std::integral_constant<int, 4>());
+  s.plan.wide == 2 ? attend(std::integral_constant<int, 2>()) : attend(std::integral_constant<int, 4>());
   if (int rc = launched("ckv_paged_attend_rows")) return rc;
   if (s.plan.places == 1) return CKV_OK;
   const long long blocks = units * s.plan.blocks, most = 32 * s.plan.wide / kRowsJoined;
   const dim3 joins((unsigned)blocks, (unsigned)std::max(1ll, std::min(most, 2048 / blocks)));
   auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, joins, dim3(32 * kRowsJoined), 0, (hipStream_t)stream, RowsCall{p, c}); };
-  s.plan.wide == 1 ? join(paged_rows_join_kernel<1>) : s.plan.wide == 2 ? join(paged_rows_join_kernel<2>) : join(paged_rows_join_kernel<4>);
+  s.plan.wide == 2 ? join(paged_rows_join_kernel<2>) : join(paged_rows_join_kernel<4>);
   return launched("ckv_paged_attend_rows");
 }
 

@@ -167,11 +167,20 @@ __device__ __forceinline__ int even_share(const Paged& p, const RowsAttend& c, i
 //   logits   K Q^T by 32 x 32 x 16 products, rows = entries, columns = the wavefront's 32 rows, so that a row's maximum and sum are a lane's own but for one exchange of halves;
 //   outputs  V^T P^T with the logits' registers as operand, entries in the order in which K Q^T leaves them, and values read out of LDS transposed (columns = rows again,
 //            so that what shrinks them is the lane's own too).
-// Weights go in as two bf16 terms (16 bits) for bf16 outputs, three for float outputs.  An entry that only some rows of the block see gives the others
+// Weights go in as two bf16 terms (16 bits) for bf16 outputs, three (24) for float outputs: 24 and 32 products for 32 entries where one term would need 16, and would be off by as much as the rounding
+// of a bf16 output where few entries weigh.  An entry that only some rows of the block see gives the others
 // nothing, whatever its value: where something that is not finite comes out the piece is done again with the finite values alone, and rows that give others weight
 // get NaN where those are.
+// What bounds it: long pieces of many rows are bound by what a SIMD can issue, half of its cycles in products and as many in what lies between (exponentials, sums, splitting weights), two wavefronts in turn:
+// prompts of 2 sequences of 8192, 40 heads, window 4096, bf16 1.43 to 1.50 ms, 1032 GFLOP at 700 TFLOP/s (1050 counting both terms; a large product reaches 1250), no bank of LDS met twice; the
+// clock falls to 2.0 .. 2.2 GHz under it.  8 bits cost the conversion: 48 rows of 40 heads over 131072 entries 230 to 238 us, 550 TFLOP/s.
+// Short pieces are bound by what comes one after another: a piece's beginning and end take 30000 cycles (lengths, mask, table, first entries, outputs), a tile of 128 rows by 32 entries 2400 alone and 3700 beside
+// another workgroup.
+// Built, measured and not kept: a step's loads between its products (loads into LDS wait their turn there too: 1.58 ms instead of 1.50), a higher priority for wavefronts that load (the same), 32 rows a workgroup with
+// 128 entries at once (128 KB of LDS: 8 bits 108 us for 8 rows of 4 heads over 4096 entries of 32 sequences where blocks of 64 rows with idle wavefronts take 83; bf16 113 and 118), 8 bits written to LDS
+// in another order of rows (the same).
 template <bool E4M3, int WIDE, int TERMS>
-__global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel(RowsCall call) {
+__global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) {
   const Paged& p = call.p;
   const RowsAttend& c = call.c;
   constexpr int kDeep = kAttendWaves / WIDE, kUnit = 32 * kDeep, NU = WIDE == 4 ? 2 : 1, kRows = 32 * WIDE, kBuf = NU * kUnit * 256;
@@ -204,7 +213,7 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
   }
   const int first = uniform_i32(span.first), count = uniform_i32(span.count), t_lo = uniform_i32((int)(r0 / c.G)), t_hi = uniform_i32((int)((min(r0 + kRows, n_rows) - 1) / c.G));
   const uint32_t row = r0 + 32 * wq + j;
-  const bool valid = row < n_rows;
+  const bool valid = row < n_rows, idle = r0 + 32 * wq >= n_rows;        // idle: a wavefront without rows only brings entries into LDS
   const int token = (int)((valid ? row : r0) / c.G), g = (int)((valid ? row : r0) - (uint32_t)token * c.G);
 
   bf16x8 q[8];                                   // (a block's rows behind the last one: its first once more, and nobody's)
@@ -636,14 +645,16 @@ __global__ __launch_bounds__(kThreads, WIDE == 1 ? 1 : 2) void paged_rows_kernel
     if (i + NU <= units) ask(std::true_type(), n + 1, buf ^ 1);
     k_at_ += buf ? kBuf : -kBuf;
     v_at_ += buf ? kBuf : -kBuf;
-    const bool whole = clear(i, NU);
-    steady(std::integral_constant<int, 0>(), i, whole, s, t, w, y);
-    if constexpr (NU == 2) {
-      steady(std::integral_constant<int, kUnit * 256>(), i + 1, whole, t, s, y, w);
-    } else {
-      s = t;
+    if (!idle) {
+      const bool whole = clear(i, NU);
+      steady(std::integral_constant<int, 0>(), i, whole, s, t, w, y);
+      if constexpr (NU == 2) {
+        steady(std::integral_constant<int, kUnit * 256>(), i + 1, whole, t, s, y, w);
+      } else {
+        s = t;
 #pragma unroll
-      for (int x = 0; x < TERMS; ++x) w[x][0] = y[x][0], w[x][1] = y[x][1];
+        for (int x = 0; x < TERMS; ++x) w[x][0] = y[x][0], w[x][1] = y[x][1];
+      }
     }
     if (i + NU > units) break;
     put(buf ^ 1);
