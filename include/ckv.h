@@ -452,7 +452,8 @@ typedef struct {
 
 /* A rotation by positions: of the first 2 n_pairs dimensions pair j turns by the angle a = position * frequencies[j] (dev double [n_pairs], radians per
  * position), (x, y) -> magnitude * (x cos a - y sin a, y cos a + x sin a); pair j is the dimensions j and j + n_pairs, or 2 j and 2 j + 1 where interleaved is 1.  The other
- * dimensions stay as they are.  n_pairs: a multiple of 8, 8 .. 64.  Angles are held in 64 bits, sines, cosines and what turns in 32. */
+ * dimensions stay as they are.  n_pairs: a multiple of 8, 8 .. 64.  Angles are held in 64 bits, and so are
+ * sines, cosines and keys on their way to 8 bits; what goes to bf16 turns in 32. */
 typedef struct {
   const double* frequencies;
   int32_t n_pairs, interleaved;

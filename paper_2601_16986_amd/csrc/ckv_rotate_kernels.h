@@ -134,10 +134,12 @@ struct Pairing {
 };
 
 // One workgroup per (sequence, KV head with its queries) and page that new rows reach, as in paged_append_kernel.  Sixteen lanes take a row: each works out the sines and
-// cosines of four pairs and gives them to those who need them, then the row's heads go by, key and value first, kAhead of them on their way at once; where the page gets
+// cosines of four pairs and gives them to those who need them, then the row's heads go by, key and value first, kTurnAhead of them on their way at once; where the page gets
 // fewer than sixteen rows, sixteen lanes take some of a row's heads.  Where pages are few, more workgroups (blockIdx.z) share a page's heads, the first of them keys and values too
 // (SHARED, turned_by; 64 rows of 4 sequences with 8 heads for each of 4 KV heads: 13.3 us by one, 9.4 by eight).
-constexpr int kTurnAhead = 4;
+// What bounds it: prompts of 8 sequences of up to 9350, 40 heads of queries, memory (1074 MB in 260 us, 4.1 TB/s; a plain copy 4.7), as long as four wavefronts per SIMD fit: with 1, 2, 3, 4 or 8 heads on their
+// way (108, 115, 125, 134, 170 registers) 299, 260, 259, 277 and 328 us.  A row of each of 32 sequences, 7.2 us, by what comes one after another: lengths, table, rows, sines and cosines, codes, bounds.
+constexpr int kTurnAhead = 2;
 template <bool E4M3, bool SHARED>
 __global__ __launch_bounds__(kThreads) void paged_append_rotated_kernel(Paged p, Rows r, Turned c) {
   const int z = SHARED ? blockIdx.z : 0;
