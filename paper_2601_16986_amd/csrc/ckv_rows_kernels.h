@@ -171,14 +171,15 @@ __device__ __forceinline__ int even_share(const Paged& p, const RowsAttend& c, i
 // of a bf16 output where few entries weigh.  An entry that only some rows of the block see gives the others
 // nothing, whatever its value: where something that is not finite comes out the piece is done again with the finite values alone, and rows that give others weight
 // get NaN where those are.
-// What bounds it: long pieces of many rows are bound by what a SIMD can issue, half of its cycles in products and as many in what lies between (exponentials, sums, splitting weights), two wavefronts in turn:
-// prompts of 2 sequences of 8192, 40 heads, window 4096, bf16 1.43 to 1.50 ms, 1032 GFLOP at 700 TFLOP/s (1050 counting both terms; a large product reaches 1250), no bank of LDS met twice; the
+// What bounds it: long pieces of many rows by their way through LDS, which each wavefront reads whole for its 32 rows, 16 KB for the 24 products of 32 entries, beside the entries that come in.  A copy that reads
+// nothing out of LDS takes 18 % less, one that loads no entries 18 % less, one without both 28 %, and then what the products alone take at their clock; the exponentials and splitting of weights fit between
+// products (3 of them 101 cycles, with all that goes with them 122; two exponentials 29, a pair packed 11, a remainder 8).  Prompts of 2 sequences of 8192, 40 heads, window 4096, bf16 1.43 to 1.50 ms, 1032 GFLOP at 700 TFLOP/s (1050 counting both terms; a large product reaches 1250), no bank of LDS met twice; the
 // clock falls to 2.0 .. 2.2 GHz under it.  8 bits cost the conversion: 48 rows of 40 heads over 131072 entries 230 to 238 us, 550 TFLOP/s.
 // Short pieces are bound by what comes one after another: a piece's beginning and end take 30000 cycles (lengths, mask, table, first entries, outputs), a tile of 128 rows by 32 entries 2400 alone and 3700 beside
 // another workgroup.
 // Built, measured and not kept: a step's loads between its products (loads into LDS wait their turn there too: 1.58 ms instead of 1.50), a higher priority for wavefronts that load (the same), 32 rows a workgroup with
 // 128 entries at once (128 KB of LDS: 8 bits 108 us for 8 rows of 4 heads over 4096 entries of 32 sequences where blocks of 64 rows with idle wavefronts take 83; bf16 113 and 118), 8 bits written to LDS
-// in another order of rows (the same).
+// in another order of rows, the next logits a turn early with their largest value beside the last outputs (both the same).
 template <bool E4M3, int WIDE, int TERMS>
 __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) {
   const Paged& p = call.p;
