@@ -87,10 +87,8 @@ struct RowsCost {
   }
 };
 
-// Which of all units' `each` blocks of rows the workgroup `index` takes: workgroups go to the eight parts of the chip in turn, each with a cache of its own, so a unit's blocks, which read the
-// same entries, go to one of them, units in turn; those of the last units that make no full round are dealt out evenly, neighbours together.  T(-1): none.  A call's pieces are so many workgroups
-// for all first ones, as many for all second ones and so on: the places that turn out to be empty come last (first to last in each unit they took workgroups' room from what there was to do:
-// 25 rows for 16 sequences in a window of 1024 69 us, not 52).
+// Which of all groups' `each` blocks of rows the workgroup `index` takes: workgroups go to the eight parts of the chip in turn, each with a cache of its own, so the blocks of a group, which read the
+// same entries (a unit's, in one piece of it), go to one of them, groups in turn; those of the last groups that make no full round are dealt out evenly, neighbours together.  T(-1): none.
 constexpr int kParts = 8;
 template <class T>
 CKV_PLAN T rows_grid(T units, T each) {
@@ -106,6 +104,17 @@ CKV_PLAN T rows_piece(T index, T units, T each) {
   }
   const T in = index - full * each, rest = (units - full) * each, chunk = (rest + kParts - 1) / kParts, at = in % kParts * chunk + in / kParts;
   return at < rest ? full * each + at : T(-1);
+}
+// The groups: all units' first pieces, then all second ones and so on, so that the places that turn out to be empty come last (first to last in each unit they took workgroups' room from what there was
+// to do: 25 rows for 16 sequences in a window of 1024 69 us, not 52).  Where units are few or make no full rounds, each piece of a unit on another part of the chip than the one before (39 rows of 3 heads for
+// 3 sequences of up to 6845 x 4 KV heads 30.6 us, all on one 43.6); else on the same, which has its queries, mask and table then (8 drafts of 4 short sequences x 4 heads 20.3 us, 21.6 on another each).
+struct RowsGroup {
+  unsigned part, unit;
+};
+CKV_PLAN RowsGroup rows_group(unsigned group, unsigned units) {
+  const unsigned part = group / units, in = group - part * units;
+  if (units % 2 || (units % kParts == 0 && units > kParts)) return {part, in};
+  return {part, (in + part) % units};
 }
 
 }  // namespace ckv

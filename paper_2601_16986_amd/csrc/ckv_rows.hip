@@ -105,7 +105,7 @@ int ckv_paged_attend_rows(const ckv_pages* pages, const ckv_seqs* seqs, const ck
     return attend_one_row(pages, seqs, &query, queries->first, mask, scale_log2e, out, out_dtype, lse, workspace, workspace_bytes, stream);
   }
   const RowsSplit s = rows_split(pages, seqs, queries->rows, queries->n_q_heads, mask, compute_units());
-  const long long units = (long long)seqs->batch * pages->n_kv_heads, grid = rows_grid(units, (long long)s.plan.blocks) * s.plan.places;
+  const long long units = (long long)seqs->batch * pages->n_kv_heads, grid = rows_grid(units * s.plan.places, (long long)s.plan.blocks);
   if (!launches(grid, kThreads) || !launches(units * s.plan.blocks, 32 * kRowsJoined)) return fail(CKV_EINVAL, "too many rows for one attention (2^24 blocks of 128, a row per query head)");
   if (s.bytes() > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < s.bytes())) return fail(CKV_EWORKSPACE, "workspace too small or misaligned");
   const Paged p = paged_of(pages, seqs);

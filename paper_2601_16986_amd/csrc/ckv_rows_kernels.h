@@ -195,9 +195,11 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i32(tid >> 6), j = lane & 31, half = lane >> 5, wq = wave % WIDE, wk = wave / WIDE;
   if (tid == 0) s_odd = 0;
-  const uint32_t each = (uint32_t)c.blocks, all = rows_grid((uint32_t)c.units, each), part_ = blockIdx.x / all, piece = rows_piece(blockIdx.x - part_ * all, (uint32_t)c.units, each);
+  const uint32_t each = (uint32_t)c.blocks, piece = rows_piece(blockIdx.x, (uint32_t)c.units * (uint32_t)c.places, each);
   if (piece == ~0u) return;
-  const int part = uniform_i32((int)part_), u = uniform_i32((int)(piece / each)), blk = uniform_i32((int)(each - 1 - (piece - u * each)));       // the last rows have the most to do
+  const uint32_t group = (uint32_t)uniform_i32((int)(piece / each));
+  const RowsGroup of = rows_group(group, (uint32_t)c.units);
+  const int part = uniform_i32((int)of.part), u = uniform_i32((int)of.unit), blk = uniform_i32((int)(each - 1 - (piece - group * each)));       // the last rows have the most to do
   const int b = uniform_i32((int)((uint32_t)u / (uint32_t)p.hkv)), h = u - b * p.hkv;
   const int64_t block_index = (int64_t)u * c.blocks + blk;
   const Told own = told(p, c.rows, b), mine = told(p, c.rows, min(lane * ((p.batch + 63) >> 6), p.batch - 1));

@@ -118,6 +118,23 @@ def test_every_block_of_rows_has_one_workgroup(tmp_path):
     }""")
 
 
+def test_every_piece_has_a_group(tmp_path):
+    """All units' first pieces come before all second ones; few units' pieces go round the chip's eight parts, those of many that make full rounds stay on one."""
+    _run(tmp_path, r"""
+  for (unsigned units : {1u, 2u, 3u, 7u, 8u, 9u, 12u, 16u, 64u, 100u, 255u})
+    for (unsigned places : {1u, 2u, 8u, 9u, 24u}) {
+      std::vector<int> on(units * places, -1);
+      for (unsigned g = 0; g < units * places; ++g) {
+        const ckv::RowsGroup r = ckv::rows_group(g, units);
+        if (r.part != g / units || r.unit >= units || on[r.part * units + r.unit] >= 0) return std::printf("group %u of %u\n", g, units), 1;
+        on[r.part * units + r.unit] = (int)(g % 8);
+      }
+      for (unsigned u = 0; u < units; ++u)
+        for (unsigned i = 1; i < places; ++i)
+          if ((on[i * units + u] == on[(i - 1) * units + u]) != (units % 8 == 0 && units > 8)) return std::printf("%u units: piece %u of %u\n", units, i, u), 1;
+    }""")
+
+
 def test_pieces_fit_their_places(tmp_path):
     """Whatever share the lengths lead to, a block has no more pieces than places, they are its tiles one after another, and a call has not many more workgroups than find room."""
     _run(tmp_path, r"""
@@ -183,7 +200,8 @@ def _queries(**how):
 
 
 def _bytes(g, rows=8, heads=8, mask=None):
-    return ckv.load().ckv_paged_rows_workspace_bytes(C.addressof(g[0]), C.addressof(g[1]), rows, heads, C.addressof(mask or ckv.Mask(0, 0, None, 0, 0)))
+    m = mask or ckv.Mask(0, 0, None, 0, 0)               # held until the call is over
+    return ckv.load().ckv_paged_rows_workspace_bytes(C.addressof(g[0]), C.addressof(g[1]), rows, heads, C.addressof(m))
 
 
 POOLS = [("n_pages", 0), ("page_size", 48), ("dtype", 0), ("k", None), ("page_stride", 0), ("scales", None)]
@@ -238,7 +256,8 @@ def test_other_arguments_of_an_attention_of_rows(good):
     lib = ckv.load()
     assert {_attend(good, scale=0.0), _attend(good, scale=float("nan")), _attend(good, scale=float("inf")), _attend(good, scale=-1.0), _attend(good, out=None), _attend(good, out=4100),
             _attend(good, dtype=ckv.E4M3), _attend(good, dtype=0)} == {ckv.EINVAL}
-    p, s, q, m = C.addressof(good[0]), C.addressof(good[1]), C.addressof(_queries()), C.addressof(ckv.Mask(0, 0, None, 0, 0))
+    queries, mask = _queries(), ckv.Mask(0, 0, None, 0, 0)
+    p, s, q, m = (C.addressof(x) for x in (good[0], good[1], queries, mask))
     for args in ((None, s, q, m), (p, None, q, m), (p, s, None, m), (p, s, q, None)):
         assert lib.ckv_paged_attend_rows(*args, 0.1, 4096, ckv.BF16, None, 4096, 1 << 40, None) == ckv.EINVAL
     assert lib.ckv_paged_rows_workspace_bytes(p, s, 8, 8, None) == 0
