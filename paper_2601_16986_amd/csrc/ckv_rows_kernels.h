@@ -130,7 +130,7 @@ __device__ __forceinline__ int even_share(const Paged& p, const RowsAttend& c, i
   auto have = [&](const Told& t) {
     const RowSpan s = c.rows.span(t.length, t.first, t.start, t.stop, p.max_length);
     if (s.count == 0) return Have{0.f, 0.f};
-    const int end = s.first + s.count, oldest = c.window ? max(s.first + (c.tree ? 0 : s.count - block_rows / c.G) - c.window, 0) : 0;
+    const int end = s.first + s.count, oldest = c.window ? max(s.first + (c.tree ? 0 : max(s.count - block_rows / c.G, 0)) - c.window, 0) : 0;
     return Have{(float)(((int64_t)s.count * c.G + block_rows - 1) / block_rows), (float)row_tiles(oldest, end, c.window ? c.sinks : 0, size).count};
   };
   Have one = {0.f, 0.f};

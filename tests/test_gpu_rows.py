@@ -139,6 +139,28 @@ def test_rows_of_the_middle():
     check_rows(f, q, out, [20, 20], first=[50, 70], lse=lse)
 
 
+@pytest.mark.parametrize("e4m3", [True, False])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (33, 0), (40, 5)])
+def test_a_single_row_anywhere(e4m3, window, sinks):
+    """One row per sequence at its first, at its last or in between; a sequence without entries, and rows that are not there; the same rows packed."""
+    lengths, first = [200, 300, 1, 0, 90, 64, 40], [50, 299, 0, 0, 0, 64, 39]
+    counts = [1, 1, 1, 0, 1, 0, 1]
+    f = Filled(lengths, 2, 16, e4m3, seed=window)
+    q = queries(f, 1, 8)
+    out = torch.full(q.shape, -77.0, device=DEV)
+    _, lse = f.cache.attend_rows(f.seqs, device(q), first=ints(first), out=out, window=window, sinks=sinks, f32=True, lse=True)
+    check_rows(f, q, out, counts, first=first, window=window, sinks=sinks, lse=lse)
+    assert (out[3] == -77.0).all() and (out[5] == -77.0).all() and f.cache.status() == 0
+    packed = torch.cat([device(q)[b, :c] for b, c in enumerate(counts)])
+    some, z = f.cache.attend_rows(f.seqs, packed, rows=1, first=ints(first), starts=ints(np.cumsum([0] + counts)), window=window, sinks=sinks, f32=True, lse=True)
+    again, zs = torch.zeros_like(out), torch.zeros_like(lse)
+    at = 0
+    for b, c in enumerate(counts):
+        again[b, :c], zs[b, :c] = some[at:at + c], z[at:at + c]
+        at += c
+    check_rows(f, q, again, counts, first=first, window=window, sinks=sinks, lse=zs)
+
+
 # ------------------------------------------------------------------ windows
 @pytest.mark.parametrize("e4m3", [True, False])
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 4), (5, 1), (16, 17), (63, 0), (64, 4), (65, 64), (100, 200), (129, 5), (500, 4), (10 ** 6, 3), (2 ** 31 - 1, 2 ** 31 - 1)])
