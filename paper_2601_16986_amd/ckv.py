@@ -712,11 +712,15 @@ class PagedCache:
         queries = turned = None
         if q is not None:
             queries = self._row_heads(seqs, q, packed, r.rows, r.total)
-            if out is None:
-                out = self.torch.empty_like(q) if q.is_contiguous() else self._like.new_empty(q.shape)
-            elif out.shape != q.shape:
-                raise CkvError(EINVAL, "out must be of q's shape")
-            turned = queries if out is q else self._row_heads(seqs, out, packed, r.rows, r.total)
+            if out is None and q.is_contiguous():
+                out = self.torch.empty_like(q)
+                turned = Heads(out.data_ptr(), queries.seq_stride, queries.row_stride, queries.head_stride, queries.n_q_heads)
+            else:
+                if out is None:
+                    out = self._like.new_empty(q.shape)
+                elif out.shape != q.shape:
+                    raise CkvError(EINVAL, "out must be of q's shape")
+                turned = queries if out is q else self._row_heads(seqs, out, packed, r.rows, r.total)
         elif out is not None:
             raise CkvError(EINVAL, "out without q")
         self._call(self.lib.ckv_paged_append_rotated, self._ref, seqs._ref, C.addressof(r), rotation._ref, at_positions, C.addressof(queries) if queries else None,
