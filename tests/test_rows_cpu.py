@@ -1,6 +1,7 @@
 """Several rows per sequence of a cache in pages without a GPU: what the definitions say of small cases, the index arithmetic of the kernels (compiled on its own), and what the entry points refuse."""
 import ctypes as C
 import os
+import re
 import shutil
 import subprocess
 
@@ -9,6 +10,7 @@ import pytest
 
 from oracle import paged as ref
 from paper_2601_16986_amd import ckv
+from tests.test_kernel_resources_cpu import _tool
 from tests.test_paged_cpu import good  # noqa: F401
 
 
@@ -172,6 +174,27 @@ def test_a_page_s_heads_are_shared_where_pages_are_few(tmp_path):
         if (by < 1 || by > group + 1 || (by > 1 && (rows <= 16 || pages * by > 256))) return std::printf("%d for %lld pages\n", by, pages), 1;
       }
   if (ckv::turned_by(32, 64, 7, 256) != 8 || ckv::turned_by(200, 64, 7, 256) != 1) return 1;""")
+
+
+def test_two_workgroups_find_room_on_a_compute_unit(tmp_path):
+    """Of its 160 KB of LDS and 512 registers a lane of each SIMD, as the share of a call's pieces counts on."""
+    fat, part, co = (str(tmp_path / x) for x in ("fat", "part", "co"))
+    subprocess.run([_tool("llvm-objcopy"), f"--dump-section=.hip_fatbin={fat}", ckv.LIB_PATH, str(tmp_path / "copy.so")], check=True)
+    with open(fat, "rb") as f:
+        bundles = f.read().split(b"__CLANG_OFFLOAD_BUNDLE__")[1:]         # one of each source
+    got = {}
+    for bundle in bundles:
+        with open(part, "wb") as f:
+            f.write(b"__CLANG_OFFLOAD_BUNDLE__" + bundle)
+        subprocess.run([_tool("clang-offload-bundler"), "--type=o", "--unbundle", f"--input={part}", "--targets=hipv4-amdgcn-amd-amdhsa--gfx950", f"--output={co}"], check=True)
+        notes = subprocess.run([_tool("llvm-readelf"), "--notes", co], check=True, capture_output=True, text=True).stdout
+        for block in re.split(r"\n  - ", notes):
+            name = re.search(r"\.name:\s+(_Z\S+)", block)
+            if name and "paged_rows_kernel" in name.group(1):
+                got[name.group(1)] = {k: int(v) for k, v in re.findall(r"\.(\w+):\s+(\d+)$", block, re.M)}
+    assert len(got) == 8
+    for n, k in got.items():
+        assert k["group_segment_fixed_size"] <= 80 * 1024 and k["vgpr_count"] <= 256, n
 
 
 # ------------------------------------------------------------------ refusals
