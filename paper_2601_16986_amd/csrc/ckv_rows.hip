@@ -142,7 +142,7 @@ int ckv_paged_attend_rows(const ckv_pages* pages, const ckv_seqs* seqs, const ck
   if (int rc = launched("ckv_paged_attend_rows")) return rc;
   if (s.plan.places == 1) return CKV_OK;
   const long long blocks = units * s.plan.blocks, most = 32 * s.plan.wide / kRowsJoined;
-  const dim3 joins((unsigned)blocks, (unsigned)std::max(1ll, std::min(most, 2048 / blocks)));
+  const dim3 joins((unsigned)blocks, (unsigned)std::max(1ll, std::min(most, 8192 / blocks)));
   auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, joins, dim3(32 * kRowsJoined), 0, (hipStream_t)stream, RowsCall{p, c}); };
   s.plan.wide == 2 ? join(paged_rows_join_kernel<2>) : join(paged_rows_join_kernel<4>);
   return launched("ckv_paged_attend_rows");

@@ -741,7 +741,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
   if (bad && a->p.status) atomicOr(a->p.status, bad);
 }
 
-// Joins the pieces of blocks of rows that have several: 32 threads a row, four dimensions each, eight rows a workgroup, which takes every `gridDim.y`-th eight of a block.
+// Joins the pieces of blocks of rows that have several: 32 threads a row, four dimensions each, eight rows a workgroup, which takes every `gridDim.y`-th eight of a block (64 drafts of 32
+// sequences of many lengths, 512 blocks: 14.6 us with all of a block's eights side by side, 19.4 with four).  Bound by trips: parts, lengths, partial outputs, eight of them at once.
 constexpr int kRowsJoined = 8;
 template <int WIDE>
 __global__ __launch_bounds__(32 * kRowsJoined) void paged_rows_join_kernel(RowsCall call) {
