@@ -174,11 +174,11 @@ __device__ __forceinline__ int even_share(const Paged& p, const RowsAttend& c, i
 // What bounds it: long pieces of many rows by what moves, in LDS's time and in power: each wavefront reads all keys and values out of LDS for its 32 rows, 16 KB for the 24 products of 32 entries, beside the
 // entries that come in.  A copy that reads nothing out of LDS takes 18 % less, one that loads no entries 18 % less, one without both 28 % (at a higher clock, too), which is what the products take; reads
 // asked for a turn earlier change nothing, so it is not their latency; the exponentials and splitting of weights fit between
-// products (3 of them 101 cycles, with all that goes with them 122; two exponentials 29, a pair packed 11, a remainder 8).  Prompts of 2 sequences of 8192, 40 heads, window 4096, bf16 1.43 to 1.50 ms, 1032 GFLOP at 700 TFLOP/s
-// (1050 counting both terms; a large product reaches 1250), no bank of LDS met twice; the clock falls to 2.0 .. 2.2 GHz under it.  8 bits cost the conversion: 48 rows of 40 heads over 131072 entries 230 to 238 us, 550 TFLOP/s.
+// products (3 of them 101 cycles, with all that goes with them 122; two exponentials 29, a pair packed 11, a remainder 8).  Prompts of 2 sequences of 8192, 40 heads, window 4096, bf16 1.43 to 1.58 ms from one card to the next, 1032 GFLOP at 700 TFLOP/s
+// (1050 counting both terms; a large product reaches 1250), no bank of LDS met twice; the clock falls to 2.0 .. 2.2 GHz under it.  8 bits cost the conversion: 48 rows of 40 heads over 131072 entries 230 to 254 us, 540 TFLOP/s.
 // Short pieces are bound by what comes one after another: a piece's beginning and end take 30000 cycles (lengths, mask, table, first entries, outputs), a tile of 128 rows by 32 entries 2400 alone and 3700 beside
 // another workgroup.
-// Built, measured and not kept: a step's loads between its products (loads into LDS wait their turn there too: 1.58 ms instead of 1.50), a higher priority for wavefronts that load (the same), 32 rows a workgroup with
+// Built, measured and not kept: a step's loads between its products (25 drafts in a window of 1024 55 us instead of 52, prompts no faster), a higher priority for wavefronts that load (the same), 32 rows a workgroup with
 // 128 entries at once (128 KB of LDS: 8 bits 108 us for 8 rows of 4 heads over 4096 entries of 32 sequences where blocks of 64 rows with idle wavefronts take 83; bf16 113 and 118), 8 bits written to LDS
 // in another order of rows, the next logits a turn early with their largest value beside the last outputs (both the same).
 template <bool E4M3, int WIDE, int TERMS>
