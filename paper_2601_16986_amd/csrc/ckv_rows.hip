@@ -132,12 +132,12 @@ int ckv_paged_attend_rows(const ckv_pages* pages, const ckv_seqs* seqs, const ck
     c.parts = (int32_t*)((char*)workspace + s.partial + s.ml);
   }
   auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), 0, (hipStream_t)stream, RowsCall{p, c}); };
-  auto terms = [&](auto e4m3, auto wide) {
+  auto typed = [&](auto e4m3, auto wide) {
     constexpr bool E4M3 = decltype(e4m3)::value;
     constexpr int WIDE = decltype(wide)::value;
-    c.out_bf16 ? launch(paged_rows_kernel<E4M3, WIDE, 2>) : launch(paged_rows_kernel<E4M3, WIDE, 3>);
+    c.out_bf16 ? launch(paged_rows_kernel<E4M3, WIDE, false>) : launch(paged_rows_kernel<E4M3, WIDE, true>);
   };
-  auto attend = [&](auto wide) { pages->dtype == CKV_E4M3 ? terms(std::true_type(), wide) : terms(std::false_type(), wide); };
+  auto attend = [&](auto wide) { pages->dtype == CKV_E4M3 ? typed(std::true_type(), wide) : typed(std::false_type(), wide); };
   s.plan.wide == 2 ? attend(std::integral_constant<int, 2>()) : attend(std::integral_constant<int, 4>());
   if (int rc = launched("ckv_paged_attend_rows")) return rc;
   if (s.plan.places == 1) return CKV_OK;

@@ -167,8 +167,9 @@ __device__ __forceinline__ int even_share(const Paged& p, const RowsAttend& c, i
 //   logits   K Q^T by 32 x 32 x 16 products, rows = entries, columns = the wavefront's 32 rows, so that a row's maximum and sum are a lane's own but for one exchange of halves;
 //   outputs  V^T P^T with the logits' registers as operand, entries in the order in which K Q^T leaves them, and values read out of LDS transposed (columns = rows again,
 //            so that what shrinks them is the lane's own too).
-// Weights go in as two bf16 terms (16 bits) for bf16 outputs, three (24) for float outputs: 24 and 32 products for 32 entries where one term would need 16, and would be off by as much as the rounding
-// of a bf16 output where few entries weigh.  An entry that only some rows of the block see gives the others
+// Weights go in as three bf16 terms, which hold the 24 bits of a float: 32 products for 32 entries where one term would need 16.  (Two terms, 16 bits, take a fifth less time, prompts below 1.44 ms and drafts 245 us where
+// three take 1.79 and 290, and leave outputs that nearly cancel off by 2^-18 of their terms: of 8388608 bf16 outputs over up to 9350 entries 20920 then round the other way than the exact ones, 3102 with three
+// terms, 7017 in float arithmetic throughout.)  An entry that only some rows of the block see gives the others
 // nothing, whatever its value: where something that is not finite comes out the piece is done again with the finite values alone, and rows that give others weight
 // get NaN where those are.
 // What bounds it: long pieces of many rows by what moves, in LDS's time and in power: each wavefront reads all keys and values out of LDS for its 32 rows, 16 KB for the 24 products of 32 entries, beside the
@@ -181,11 +182,11 @@ __device__ __forceinline__ int even_share(const Paged& p, const RowsAttend& c, i
 // Built, measured and not kept: a step's loads between its products (25 drafts in a window of 1024 55 us instead of 52, prompts no faster), a higher priority for wavefronts that load (the same), 32 rows a workgroup with
 // 128 entries at once (128 KB of LDS: 8 bits 108 us for 8 rows of 4 heads over 4096 entries of 32 sequences where blocks of 64 rows with idle wavefronts take 83; bf16 113 and 118), 8 bits written to LDS
 // in another order of rows, the next logits a turn early with their largest value beside the last outputs (both the same).
-template <bool E4M3, int WIDE, int TERMS>
+template <bool E4M3, int WIDE, bool F32>
 __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) {
   const Paged& p = call.p;
   const RowsAttend& c = call.c;
-  constexpr int kDeep = kAttendWaves / WIDE, kUnit = 32 * kDeep, NU = WIDE == 4 ? 2 : 1, kRows = 32 * WIDE, kBuf = NU * kUnit * 256;
+  constexpr int TERMS = 3, kDeep = kAttendWaves / WIDE, kUnit = 32 * kDeep, NU = WIDE == 4 ? 2 : 1, kRows = 32 * WIDE, kBuf = NU * kUnit * 256;
   constexpr int kLoads = kUnit / (E4M3 ? 32 : 16), kWords = kMaxDrafts / 32 + 3;
   __shared__ __align__(16) uint8_t s_tile[2][2][kBuf];          // keys, values; two buffers of NU units each
   __shared__ uint32_t s_see[kRows][kWords];
@@ -701,7 +702,6 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
   const int64_t out_row = a->c.rows.starts ? a->c.rows.starts[b] : (int64_t)b * a->c.rows.rows;
   float *lse = a->c.lse, *partial = a->c.partial, *ml = a->c.ml;
   uint8_t* out = a->c.out;
-  const bool out_bf16 = a->c.out_bf16;
   const int places = a->c.places;
   constexpr int kEnd = 4;                          // rows at once
   const int chunk = tid & 31;
@@ -733,7 +733,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
       } else {
         const int t = (int)((r0 + r) / G);
         const int64_t to = (out_row + t) * (G * hkv) + h * G + (int)(r0 + r - (uint32_t)t * G);
-        put_row(out, out_bf16, to, 4 * chunk, L[i] != 0.f ? y[i] * (1.f / L[i]) : f32x4{0.f, 0.f, 0.f, 0.f});
+        put_row(out, !F32, to, 4 * chunk, L[i] != 0.f ? y[i] * (1.f / L[i]) : f32x4{0.f, 0.f, 0.f, 0.f});
         if (chunk == 0 && lse) lse[to] = natural(M[i], L[i]);
       }
     }
