@@ -87,6 +87,15 @@ struct RowsCost {
   }
 };
 
+// What a piece's outputs, before they are divided by the sum of weights, may reach without care: kLargeSums times that (more than a block of rows has pieces) is 2^128.
+constexpr float kLargeSum = 0x1p115f, kLargeSums = 0x1p13f;
+// By what weights of at most 2^8 each are multiplied where they reach it: as many of them as a sequence has entries then add up to less than a half, and their sum times any values is finite.
+CKV_PLAN float lowered_by(int max_length) {
+  float f = 0x1p-10f;
+  for (; max_length > 1; max_length = max_length / 2 + max_length % 2) f *= 0.5f;
+  return f;
+}
+
 // Which of all groups' `each` blocks of rows the workgroup `index` takes: workgroups go to the eight parts of the chip in turn, each with a cache of its own, so the blocks of a group, which read the
 // same entries (a unit's, in one piece of it), go to one of them, groups in turn; those of the last groups that make no full round are dealt out evenly, neighbours together.  T(-1): none.
 constexpr int kParts = 8;

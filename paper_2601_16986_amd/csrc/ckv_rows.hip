@@ -126,6 +126,7 @@ int ckv_paged_attend_rows(const ckv_pages* pages, const ckv_seqs* seqs, const ck
   c.least = s.plan.least;
   c.places = s.plan.places;
   c.workers = s.plan.workers;
+  c.lower = lowered_by(seqs->max_length);
   if (s.plan.places > 1) {
     c.partial = (float*)workspace;
     c.ml = (float*)((char*)workspace + s.partial);

@@ -27,6 +27,7 @@ struct RowsAttend {
   float scale_log2e;
   int32_t G, window, sinks, out_bf16;
   int32_t blocks, least, places, workers;  // RowsPlan
+  float lower;               // lowered_by(): what weights are multiplied by where sums would be infinite
 };
 
 struct RowsCall {
@@ -171,7 +172,8 @@ __device__ __forceinline__ int even_share(const Paged& p, const RowsAttend& c, i
 // three take 1.79 and 290, and leave outputs that nearly cancel off by 2^-18 of their terms: of 8388608 bf16 outputs over up to 9350 entries 20920 then round the other way than the exact ones, 3102 with three
 // terms, 7017 in float arithmetic throughout.)  An entry that only some rows of the block see gives the others
 // nothing, whatever its value: where something that is not finite comes out the piece is done again with the finite values alone, and rows that give others weight
-// get NaN where those are.
+// get NaN where those are.  Where finite values add up to 2^115 it is done once more with lowered weights (lowered_by), whose sums stay finite; the sum of weights, which is not lowered, then has a sign
+// for the join.  (What only these ways need is what the variants of 8 bits keep in scratch, 16 and 8 registers: written before the first tile, read where a piece is done again.)
 // What bounds it: long pieces of many rows by what moves, in LDS's time and in power: each wavefront reads all keys and values out of LDS for its 32 rows, 16 KB for the 24 products of 32 entries, beside the
 // entries that come in.  A copy that reads nothing out of LDS takes 18 % less, one that loads no entries 18 % less, one without both 28 % (at a higher clock, too), which is what the products take; reads
 // asked for a turn earlier change nothing, so it is not their latency; the exponentials and splitting of weights fit between
@@ -191,11 +193,11 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
   __shared__ __align__(16) uint8_t s_tile[2][2][kBuf];          // keys, values; two buffers of NU units each
   __shared__ uint32_t s_see[kRows][kWords];
   __shared__ float s_m[kAttendWaves][32], s_l[kAttendWaves][32];
-  __shared__ int s_odd;
+  __shared__ int s_odd, s_far;
   static_assert(sizeof s_tile >= kAttendWaves * 32 * kDim * 4, "the outputs go where the tiles were");
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i32(tid >> 6), j = lane & 31, half = lane >> 5, wq = wave % WIDE, wk = wave / WIDE;
-  if (tid == 0) s_odd = 0;
+  if (tid == 0) s_odd = s_far = 0;
   const uint32_t each = (uint32_t)c.blocks, piece = rows_piece(blockIdx.x, (uint32_t)c.units * (uint32_t)c.places, each);
   if (piece == ~0u) return;
   const uint32_t group = (uint32_t)uniform_i32((int)(piece / each));
@@ -566,7 +568,9 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
   };
   f32x16 s, t;
   u32x4 w[TERMS][2], y[TERMS][2];
-  // The same with care: a unit's values that are not finite reach those rows only that give them weight.
+  // The same with care: a unit's values that are not finite reach those rows only that give them weight, and weights are `lowered`, after they have gone into their sum, so that all
+  // else stays bit by bit what it was.
+  float lowered = 1.f;
   auto any = [&](int i, int at) CKV_INLINE {
     if (i >= 1 && i <= units) {
 #pragma unroll
@@ -613,6 +617,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
         float a = fast_exp2(fmaf(s[2 * n], scale_log2e, -m)), z = fast_exp2(fmaf(s[2 * n + 1], scale_log2e, -m));
         sum += a;
         sum += z;
+        a *= lowered;
+        z *= lowered;
 #pragma unroll
         for (int x = 0; x < TERMS; ++x) {
           w[x][n >> 2][n & 3] = bf16_pack(a, z);
@@ -665,25 +671,40 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
     put(buf ^ 1);
   }
   __syncthreads();
-  // Once more with care where a page was missing, or something that is no number came out: a value that only some rows see must not reach the others.
+  // Once more with care where a page was missing, or something that is no number came out: a value that only some rows see must not reach the others.  And once more with lowered weights where finite
+  // values, of up to 2^128, add up to so much that a few thousand pieces' sums might be infinite.
   float nothing = 0.f;
 #pragma unroll
   for (int d = 0; d < 4; ++d)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) nothing = fmaf(acc[d][i], 0.f, nothing);
-  if (!(nothing == 0.f)) s_odd = 1;
+    for (int i = 0; i < 16; ++i) nothing = fmaf(acc[d][i], kLargeSums, nothing);
+  if (!(fabsf(nothing) < INFINITY)) s_odd = 1;
   __syncthreads();
   if (uniform_i32(s_odd)) {
     apart();
-    begin();
-    k_at_ = k_at0, v_at_ = v_at0;
 #pragma unroll 1
-    for (int n = -1; NU * n <= units; ++n) {
-      const int buf = n & 1;
-      ask(std::false_type(), n + 1, buf ^ 1);
+    for (int turn = 0; turn < 2; ++turn) {
+      if (turn == 1) {
+        float most = 0.f;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(acc[d][i]));
+        if (most >= kLargeSum) s_far = 1;
+        __syncthreads();
+        if (!uniform_i32(s_far)) break;
+        lowered = args()->c.lower;
+      }
+      begin();
+      k_at_ = k_at0, v_at_ = v_at0;
 #pragma unroll 1
-      for (int x = 0; x < NU; ++x) any(NU * n + x, buf * kBuf + x * kUnit * 256);
-      put(buf ^ 1);
+      for (int n = -1; NU * n <= units; ++n) {
+        const int buf = n & 1;
+        ask(std::false_type(), n + 1, buf ^ 1);
+#pragma unroll 1
+        for (int x = 0; x < NU; ++x) any(NU * n + x, buf * kBuf + x * kUnit * 256);
+        put(buf ^ 1);
+      }
     }
   }
 
@@ -703,6 +724,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
   float *lse = a->c.lse, *partial = a->c.partial, *ml = a->c.ml;
   uint8_t* out = a->c.out;
   const int places = a->c.places;
+  const float raised = 1.f / lowered;
   constexpr int kEnd = 4;                          // rows at once
   const int chunk = tid & 31;
   for (int r_first = tid >> 5; r_first < kRows; r_first += kThreads / 32 * kEnd) {
@@ -729,11 +751,11 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
       if (parts > 1) {
         const int64_t at = (block_index * places + part) * kRows + r;
         *reinterpret_cast<f32x4*>(partial + at * kDim + 4 * chunk) = y[i];
-        if (chunk == 0) *reinterpret_cast<f32x2*>(ml + 2 * at) = f32x2{M[i], L[i]};
+        if (chunk == 0) *reinterpret_cast<f32x2*>(ml + 2 * at) = f32x2{M[i], lowered < 1.f ? -L[i] : L[i]};
       } else {
         const int t = (int)((r0 + r) / G);
         const int64_t to = (out_row + t) * (G * hkv) + h * G + (int)(r0 + r - (uint32_t)t * G);
-        put_row(out, !F32, to, 4 * chunk, L[i] != 0.f ? y[i] * (1.f / L[i]) : f32x4{0.f, 0.f, 0.f, 0.f});
+        put_row(out, !F32, to, 4 * chunk, L[i] != 0.f ? y[i] * (1.f / L[i]) * raised : f32x4{0.f, 0.f, 0.f, 0.f});
         if (chunk == 0 && lse) lse[to] = natural(M[i], L[i]);
       }
     }
@@ -759,7 +781,7 @@ __global__ __launch_bounds__(32 * kRowsJoined) void paged_rows_join_kernel(RowsC
   for (int in = blockIdx.y * kRowsJoined + (threadIdx.x >> 5); in < kRows; in += kRowsJoined * gridDim.y) {
     const uint32_t row = (uint32_t)blk * kRows + in;
     if (row >= (uint32_t)span.count * (uint32_t)c.G) return;
-    float M = kNoLogit, L = 0.f;
+    float M = kNoLogit, L = 0.f, lowered = 1.f;       // what y, of several parts, is multiplied by
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
     constexpr int N = 8;                           // parts on their way at once
     for (int i0 = 0; i0 < parts; i0 += N) {
@@ -772,8 +794,10 @@ __global__ __launch_bounds__(32 * kRowsJoined) void paged_rows_join_kernel(RowsC
         x[i] = *reinterpret_cast<const f32x4*>(c.partial + at * kDim + d4);
       }
       float m = M;
+      uint32_t signs = 0u;                         // of a part with lowered weights the sum of weights has a sign
 #pragma unroll
-      for (int i = 0; i < N; ++i) m = fmaxf(m, st[i][0]);
+      for (int i = 0; i < N; ++i) m = fmaxf(m, st[i][0]), signs |= __float_as_uint(st[i][1]);
+      if (signs >> 31 && lowered == 1.f) lowered = c.lower, y = y * lowered;
       const float old = fast_exp2(M - m);
       M = m;
       L *= old;
@@ -781,13 +805,13 @@ __global__ __launch_bounds__(32 * kRowsJoined) void paged_rows_join_kernel(RowsC
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const float now = i0 + i < parts ? fast_exp2(st[i][0] - m) : 0.f;
-        L += st[i][1] * now;
-        y += x[i] * now;
+        L += fabsf(st[i][1]) * now;
+        y += x[i] * (__float_as_uint(st[i][1]) >> 31 ? now : now * lowered);
       }
     }
     const int t = (int)(row / c.G);
     const int64_t to = ((c.rows.starts ? c.rows.starts[b] : (int64_t)b * c.rows.rows) + t) * (c.G * p.hkv) + h * c.G + (int)(row - (uint32_t)t * c.G);
-    put_row(c.out, c.out_bf16, to, d4, L != 0.f ? y * (1.f / L) : f32x4{0.f, 0.f, 0.f, 0.f});
+    put_row(c.out, c.out_bf16, to, d4, L != 0.f ? y * (1.f / L) * (1.f / lowered) : f32x4{0.f, 0.f, 0.f, 0.f});
     if (d4 == 0 && c.lse) c.lse[to] = natural(M, L);
   }
 }
