@@ -91,7 +91,8 @@ int attend(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_query* query,
   if (!s.plan.split) return CKV_OK;
   const unsigned units = (unsigned)(seqs->batch * pages->n_kv_heads);
   const int heads = (int)units > compute_units() ? std::min(G, kJoinRows) : 1;
-  hipLaunchKernelGGL(paged_join_kernel, dim3(units, (unsigned)((G + heads - 1) / heads)), dim3(32 * kJoinRows), 0, (hipStream_t)stream, c, heads);
+  auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(units, (unsigned)((G + heads - 1) / heads)), dim3(32 * kJoinRows), 0, (hipStream_t)stream, c, heads); };
+  window ? join(paged_join_kernel<true>) : join(paged_join_kernel<false>);
   return launched(what);
 }
 
@@ -107,6 +108,7 @@ int attend_one_row(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_query
   c.first = first;
   c.window = mask->window;
   c.sinks = mask->sinks;
+  c.lower = lowered_by(seqs->max_length);
   return attend(pages, seqs, query, split_window(pages, seqs, query->n_q_heads, mask, compute_units()), c, true, scale_log2e, out, out_dtype, lse, workspace, workspace_bytes, stream,
                 "ckv_paged_attend_rows");
 }

@@ -129,6 +129,7 @@ struct Attend {
   int32_t share, places, workers;          // AttendPlan
   const int32_t* first;      // WINDOW: the tokens' positions, or NULL: the sequences' last
   int32_t window, sinks;     // WINDOW: entries that a token looks back to, itself included, and first ones
+  float lower;               // WINDOW: lowered_by(), what weights are multiplied by where sums would be infinite
 };
 
 // What one token looks at: all entries of its sequence or, WINDOW, those up to its own position, of which only the last `window` and the first `sinks` count.
@@ -162,6 +163,28 @@ __device__ __forceinline__ void interleave_bytes(uint32_t a, uint32_t b, uint32_
 __device__ __forceinline__ void put_out(const Attend& c, int64_t row, int d4, f32x4 y) {
   if (c.out_bf16) *reinterpret_cast<u32x2*>(c.out + (row * kDim + d4) * 2) = u32x2{bf16_pack(y[0], y[1]), bf16_pack(y[2], y[3])};
   else *reinterpret_cast<f32x4*>(c.out + (row * kDim + d4) * 4) = y;
+}
+
+// Sums of weights of which some, those with a sign, belong to outputs of lowered weights: all outputs are then taken as lowered.
+template <bool WINDOW>
+struct Lowered {
+  float by = 1.f;
+  template <class... T>
+  __device__ __forceinline__ Lowered(const Attend& c, T... l) {
+    if constexpr (WINDOW)
+      if (((0u | ... | __float_as_uint(l)) >> 31) != 0u) by = c.lower;
+  }
+  __device__ __forceinline__ bool any() const { return WINDOW && by < 1.f; }
+  __device__ __forceinline__ float size(float l) const { return WINDOW ? fabsf(l) : l; }
+  __device__ __forceinline__ float factor(float l, float f) const { return WINDOW && !(__float_as_uint(l) >> 31) ? f * by : f; }
+  __device__ __forceinline__ f32x4 raise(f32x4 y) const { return WINDOW ? y * (1.f / by) : y; }
+};
+// All ones in each half (a bf16 number) that is not finite.
+__device__ __forceinline__ u32x4 not_finite(u32x4 x) {
+  u32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = ((x[i] & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((x[i] & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+  return r;
 }
 
 // The piece that a workgroup takes.  Where lengths decide how the work is cut they are only known here, so every workgroup looks for its own; a lane adds up its
@@ -299,141 +322,199 @@ __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend 
   for (int dt = 0; dt < 8; ++dt) acc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m_run = kNoLogit, l_run = 0.f;
 
-  for (int in = pc.first + wave; in < pc.last; in += kWaves) {
-    const int blk = block(in);
-    if (blk >> (shift + 1) != window) {
-      window = blk >> (shift + 1);
-      look_up();
-    }
-    int valid[2];
-    float sv[8], vs[8];
-    u32x4 kf[2][2][kParts], vf[2][4];
-    u32x2 sc[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int e = (blk << 5) + 16 * t, off = e & ((1 << shift) - 1), at = (e >> shift) & (kPageSlots - 1);
-      valid[t] = min(max(__builtin_amdgcn_readlane(fill, at) - off, 0), 16);
-      const int64_t pg = __builtin_amdgcn_readlane(page, at);
-      const int64_t base = pg * p.page_stride + h * p.head_stride + (int64_t)off * p.slot_stride;
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const uint8_t* kb = p.k + base + (4 * (j >> 2) + ((j >> 1) & 1) + 2 * n) * p.slot_stride + 16 * (2 * kg + (j & 1));
-#pragma unroll
-        for (int s = 0; s < kParts; ++s) kf[t][n][s] = stream16(kb + 128 * s);
+  float lowered = 1.f;
+  auto blocks = [&](auto careful) __attribute__((always_inline)) {
+    constexpr bool CAREFUL = decltype(careful)::value;
+    for (int in = pc.first + wave; in < pc.last; in += kWaves) {
+      const int blk = block(in);
+      if (blk >> (shift + 1) != window) {
+        window = blk >> (shift + 1);
+        look_up();
       }
-      const uint8_t* vb = p.v + base + 4 * kg * p.slot_stride;
+      int valid[2];
+      float sv[8], vs[8];
+      u32x4 kf[2][2][kParts], vf[2][4];
+      u32x2 sc[2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (E4M3) {
-          const u32x2 x = stream8(vb + i * p.slot_stride + 8 * j);
-          vf[t][i] = u32x4{x[0], x[1], 0u, 0u};
-        } else {
-          vf[t][i] = stream16(vb + i * p.slot_stride + 16 * j);
+      for (int t = 0; t < 2; ++t) {
+        const int e = (blk << 5) + 16 * t, off = e & ((1 << shift) - 1), at = (e >> shift) & (kPageSlots - 1);
+        valid[t] = min(max(__builtin_amdgcn_readlane(fill, at) - off, 0), 16);
+        const int64_t pg = __builtin_amdgcn_readlane(page, at);
+        const int64_t base = pg * p.page_stride + h * p.head_stride + (int64_t)off * p.slot_stride;
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          const uint8_t* kb = p.k + base + (4 * (j >> 2) + ((j >> 1) & 1) + 2 * n) * p.slot_stride + 16 * (2 * kg + (j & 1));
+#pragma unroll
+          for (int s = 0; s < kParts; ++s) kf[t][n][s] = stream16(kb + 128 * s);
         }
-      }
-      if constexpr (E4M3) sc[t] = load8(p.scales + pg * p.scale_page_stride + h * p.scale_head_stride + 2 * off + 8 * kg);      // (through the caches: a line serves several blocks)
-    }
-    // ---- logits of four entries of each tile
+        const uint8_t* vb = p.v + base + 4 * kg * p.slot_stride;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      float dot[4];
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          u32x4 x;
+        for (int i = 0; i < 4; ++i) {
           if constexpr (E4M3) {
-            const uint32_t lo = kf[t][n][0][2 * s], hi = kf[t][n][0][2 * s + 1];
-            x = u32x4{codes_bf16<false>(lo, 1.f), codes_bf16<true>(lo, 1.f), codes_bf16<false>(hi, 1.f), codes_bf16<true>(hi, 1.f)};
+            const u32x2 x = stream8(vb + i * p.slot_stride + 8 * j);
+            vf[t][i] = u32x4{x[0], x[1], 0u, 0u};
           } else {
-            x = kf[t][n][s];
+            vf[t][i] = stream16(vb + i * p.slot_stride + 16 * j);
           }
-          s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), q[s], s0, 0, 0, 0);
-          s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), q[2 + s], s1, 0, 0, 0);
         }
-        dot[2 * n] = s0[0] + s1[1];
-        dot[2 * n + 1] = s0[2] + s1[3];
+        if constexpr (E4M3) sc[t] = load8(p.scales + pg * p.scale_page_stride + h * p.scale_head_stride + 2 * off + 8 * kg);      // (through the caches: a line serves several blocks)
       }
+      // ---- logits of four entries of each tile
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float k_scale = c.scale_log2e;
-        vs[4 * t + i] = 1.f;
-        if constexpr (E4M3) {
-          const uint32_t x = sc[t][i >> 1];
-          k_scale *= __uint_as_float(i & 1 ? (x & 0xFF0000u) << 7 : (x & 0xFFu) << 23);
-          vs[4 * t + i] = __uint_as_float(i & 1 ? (x & 0xFF000000u) >> 1 : (x & 0xFF00u) << 15);
-        }
-        sv[4 * t + i] = dot[i] * k_scale;
-      }
-    }
-    // ---- entries that are not there, or not looked at: logits of -inf, values and their scales of nothing (the rows may hold anything)
-    if (valid[0] + valid[1] < 32 || (WINDOW && blk << 5 < oldest && (blk + 1) << 5 > c.sinks)) {
+      for (int t = 0; t < 2; ++t) {
+        float dot[4];
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+        for (int n = 0; n < 2; ++n) {
+          f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (const int e = (blk << 5) + 16 * t + 4 * kg + i; 4 * kg + i >= valid[t] || (WINDOW && e < oldest && e >= c.sinks)) {
-            sv[4 * t + i] = -INFINITY;
-            vs[4 * t + i] = 0.f;
-            vf[t][i] = u32x4{0u, 0u, 0u, 0u};
+          for (int s = 0; s < 2; ++s) {
+            u32x4 x;
+            if constexpr (E4M3) {
+              const uint32_t lo = kf[t][n][0][2 * s], hi = kf[t][n][0][2 * s + 1];
+              x = u32x4{codes_bf16<false>(lo, 1.f), codes_bf16<true>(lo, 1.f), codes_bf16<false>(hi, 1.f), codes_bf16<true>(hi, 1.f)};
+            } else {
+              x = kf[t][n][s];
+            }
+            s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), q[s], s0, 0, 0, 0);
+            s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), q[2 + s], s1, 0, 0, 0);
           }
-    }
-    // ---- softmax with a running maximum
-    float bm = fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])), fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7])));
-    bm = rows_combine(bm, [](float x, float y) { return fmaxf(x, y); });
-    if (__any(bm > m_run)) {
-      const float m_new = fmaxf(m_run, bm), shrink = fast_exp2(m_run - m_new);
-      l_run *= shrink;
-      m_run = m_new;
-      float f[4];
+          dot[2 * n] = s0[0] + s1[1];
+          dot[2 * n + 1] = s0[2] + s1[3];
+        }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) f[i] = __shfl(shrink, 4 * kg + i);
-#pragma unroll
-      for (int dt = 0; dt < 8; ++dt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[dt][i] *= f[i];
-    }
-    bf16x8 w[kTerms];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float weight = fast_exp2(sv[i] - m_run);
-      l_run += weight;
-      float rest = E4M3 ? weight * vs[i] : weight;
-#pragma unroll
-      for (int n = 0; n < kTerms; ++n) {
-        w[n][i] = (__bf16)rest;
-        rest -= (float)w[n][i];
-      }
-    }
-    if constexpr (!WIDE) {
-      const bool low = j >= 8;
-      const u32x4 a = __builtin_bit_cast(u32x4, w[0]), z = __builtin_bit_cast(u32x4, w[1]), y = __builtin_bit_cast(u32x4, w[2]);
-      w[0] = __builtin_bit_cast(bf16x8, u32x4{low ? z[0] : a[0], low ? z[1] : a[1], low ? z[2] : a[2], low ? z[3] : a[3]});
-      w[1] = __builtin_bit_cast(bf16x8, u32x4{low ? 0u : y[0], low ? 0u : y[1], low ? 0u : y[2], low ? 0u : y[3]});
-    }
-    // ---- weights times values: dimension 8 j + dt
-#pragma unroll
-    for (int d2 = 0; d2 < 4; ++d2) {
-      u32x4 x[2];                                      // dimensions 2 d2 and 2 d2 + 1, pairs of entries
-#pragma unroll
-      for (int pair = 0; pair < 4; ++pair) {
-        const u32x4 a = vf[pair >> 1][2 * (pair & 1)], z = vf[pair >> 1][2 * (pair & 1) + 1];
-        if constexpr (E4M3) {
-          uint32_t y[2];
-          interleave_bytes(a[d2 >> 1], z[d2 >> 1], y);
-          x[0][pair] = codes_bf16<false>(y[d2 & 1], 1.f);
-          x[1][pair] = codes_bf16<true>(y[d2 & 1], 1.f);
-        } else {
-          x[0][pair] = __builtin_amdgcn_perm(z[d2], a[d2], 0x05040100u);
-          x[1][pair] = __builtin_amdgcn_perm(z[d2], a[d2], 0x07060302u);
+        for (int i = 0; i < 4; ++i) {
+          float k_scale = c.scale_log2e;
+          vs[4 * t + i] = 1.f;
+          if constexpr (E4M3) {
+            const uint32_t x = sc[t][i >> 1];
+            k_scale *= __uint_as_float(i & 1 ? (x & 0xFF0000u) << 7 : (x & 0xFFu) << 23);
+            vs[4 * t + i] = __uint_as_float(i & 1 ? (x & 0xFF000000u) >> 1 : (x & 0xFF00u) << 15);
+          }
+          sv[4 * t + i] = dot[i] * k_scale;
         }
       }
+      // ---- entries that are not there, or not looked at: logits of -inf, values and their scales of nothing (the rows may hold anything)
+      if (valid[0] + valid[1] < 32 || (WINDOW && blk << 5 < oldest && (blk + 1) << 5 > c.sinks)) {
 #pragma unroll
-      for (int n = 0; n < (WIDE ? kTerms : kTerms - 1); ++n)
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-          acc[2 * d2 + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[n], __builtin_bit_cast(bf16x8, x[i]), acc[2 * d2 + i], 0, 0, 0);
+          for (int i = 0; i < 4; ++i)
+            if (const int e = (blk << 5) + 16 * t + 4 * kg + i; 4 * kg + i >= valid[t] || (WINDOW && e < oldest && e >= c.sinks)) {
+              sv[4 * t + i] = -INFINITY;
+              vs[4 * t + i] = 0.f;
+              vf[t][i] = u32x4{0u, 0u, 0u, 0u};
+            }
+      }
+      if constexpr (CAREFUL && E4M3) {                   // codes times 2^120 that are infinite as bf16
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (vs[i] == 0x1p120f) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n) vf[i >> 2][i & 3][n] |= ((((vf[i >> 2][i & 3][n] & 0x7F7F7F7Fu) + 0x08080808u) & 0x80808080u) >> 7) * 0x7Fu;
+          }
+      }
+      // ---- softmax with a running maximum
+      float bm = fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])), fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7])));
+      bm = rows_combine(bm, [](float x, float y) { return fmaxf(x, y); });
+      if (__any(bm > m_run)) {
+        const float m_new = fmaxf(m_run, bm), shrink = fast_exp2(m_run - m_new);
+        l_run *= shrink;
+        m_run = m_new;
+        float f[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = __shfl(shrink, 4 * kg + i);
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[dt][i] *= f[i];
+      }
+      bf16x8 w[kTerms], some;                            // some: careful, 1 where there is a weight
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float weight = fast_exp2(sv[i] - m_run);
+        l_run += weight;
+        float rest = E4M3 ? weight * vs[i] : weight;
+        if constexpr (CAREFUL) some[i] = (__bf16)(weight != 0.f ? 1.f : 0.f), rest *= lowered;
+#pragma unroll
+        for (int n = 0; n < kTerms; ++n) {
+          w[n][i] = (__bf16)rest;
+          rest -= (float)w[n][i];
+        }
+      }
+      if constexpr (!WIDE) {
+        const bool low = j >= 8;
+        const u32x4 a = __builtin_bit_cast(u32x4, w[0]), z = __builtin_bit_cast(u32x4, w[1]), y = __builtin_bit_cast(u32x4, w[2]);
+        w[0] = __builtin_bit_cast(bf16x8, u32x4{low ? z[0] : a[0], low ? z[1] : a[1], low ? z[2] : a[2], low ? z[3] : a[3]});
+        w[1] = __builtin_bit_cast(bf16x8, u32x4{low ? 0u : y[0], low ? 0u : y[1], low ? 0u : y[2], low ? 0u : y[3]});
+      }
+      // ---- weights times values: dimension 8 j + dt
+#pragma unroll
+      for (int d2 = 0; d2 < 4; ++d2) {
+        u32x4 x[2];                                      // dimensions 2 d2 and 2 d2 + 1, pairs of entries
+#pragma unroll
+        for (int pair = 0; pair < 4; ++pair) {
+          const u32x4 a = vf[pair >> 1][2 * (pair & 1)], z = vf[pair >> 1][2 * (pair & 1) + 1];
+          if constexpr (E4M3) {
+            uint32_t y[2];
+            interleave_bytes(a[d2 >> 1], z[d2 >> 1], y);
+            x[0][pair] = codes_bf16<false>(y[d2 & 1], 1.f);
+            x[1][pair] = codes_bf16<true>(y[d2 & 1], 1.f);
+          } else {
+            x[0][pair] = __builtin_amdgcn_perm(z[d2], a[d2], 0x05040100u);
+            x[1][pair] = __builtin_amdgcn_perm(z[d2], a[d2], 0x07060302u);
+          }
+        }
+        f32x4 wrong[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        if constexpr (CAREFUL) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const u32x4 ones = not_finite(x[i]);
+            wrong[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(some, __builtin_bit_cast(bf16x8, ones & 0x3F803F80u), wrong[i], 0, 0, 0);
+            x[i] &= ~ones;
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < (WIDE ? kTerms : kTerms - 1); ++n)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            acc[2 * d2 + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[n], __builtin_bit_cast(bf16x8, x[i]), acc[2 * d2 + i], 0, 0, 0);
+        if constexpr (CAREFUL) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (wrong[i][e] != 0.f) acc[2 * d2 + i][e] = NAN;
+        }
+      }
+    }
+  };
+  blocks(std::false_type());
+  if constexpr (WINDOW) {
+    // With care where something that is no number came out, so that values reach those heads only that give them weight; then with lowered weights too where
+    // finite values add up to so much that pieces' sums might be infinite.
+    float nothing = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) nothing = fmaf(acc[dt][i], kLargeSums, nothing);
+    if (__any(!(fabsf(nothing) < INFINITY))) {
+      asm volatile("");                                    // keeps this in the branch
+#pragma unroll 1
+      for (int turn = 0; turn < 2; ++turn) {
+        if (turn == 1) {
+          float most = 0.f;
+#pragma unroll
+          for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(acc[dt][i]));
+          if (!__any(most >= kLargeSum)) break;
+          lowered = c.lower;
+        }
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) acc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        m_run = kNoLogit, l_run = 0.f;
+        blocks(std::true_type());
+      }
     }
   }
 
@@ -441,7 +522,7 @@ __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend 
   l_run = rows_combine(l_run, [](float x, float y) { return x + y; });
   if (lane < 16) {
     s_m[wave][lane] = m_run;
-    s_l[wave][lane] = l_run;
+    s_l[wave][lane] = WINDOW && lowered < 1.f ? -l_run : l_run;          // of lowered weights the sum, which is not lowered, has a sign
   }
   if constexpr (!WIDE) {
 #pragma unroll
@@ -464,22 +545,23 @@ __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend 
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) M = fmaxf(M, s_m[w][head]);
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    const Lowered<WINDOW> all(c, s_l[0][head], s_l[1][head], s_l[2][head], s_l[3][head]);
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       const float f = fast_exp2(s_m[w][head] - M);
-      L += s_l[w][head] * f;
-      y += *reinterpret_cast<const f32x4*>(&s_acc[w][head * kRow + d4]) * f;
+      L += all.size(s_l[w][head]) * f;
+      y += *reinterpret_cast<const f32x4*>(&s_acc[w][head * kRow + d4]) * all.factor(s_l[w][head], f);
     }
     if (pc.parts > 1) {
       const int64_t at = (int64_t)pc.index * c.G + head;
       *reinterpret_cast<f32x4*>(c.partial + at * kDim + d4) = y;
       if (d4 == 0) {
         c.ml[2 * at] = M;
-        c.ml[2 * at + 1] = L;
+        c.ml[2 * at + 1] = all.any() ? -L : L;
       }
     } else if (!WINDOW || end > 0) {
       const int64_t row = (int64_t)u * c.G + head;
-      put_out(c, row, d4, L != 0.f ? y * (1.f / L) : f32x4{0.f, 0.f, 0.f, 0.f});
+      put_out(c, row, d4, L != 0.f ? all.raise(y * (1.f / L)) : f32x4{0.f, 0.f, 0.f, 0.f});
       if (d4 == 0 && c.lse) c.lse[row] = natural(M, L);
     }
   }
@@ -494,6 +576,7 @@ __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend 
 // parts at a time.  2.6 .. 4.7 us, of which a launch and three trips to memory are most.  (The last workgroup to arrive at a counter joining instead, with accesses past the
 // caches: the same times or 2 us more, and the counters would have to be zero before.)
 constexpr int kJoinRows = 8;
+template <bool WINDOW>
 __global__ __launch_bounds__(32 * kJoinRows) void paged_join_kernel(Attend c, int heads) {
   __shared__ float s_m[kJoinRows], s_l[kJoinRows];
   __shared__ __align__(16) float s_y[kJoinRows][kDim];
@@ -502,6 +585,7 @@ __global__ __launch_bounds__(32 * kJoinRows) void paged_join_kernel(Attend c, in
   if (parts == 1) return;
   float M = kNoLogit, L = 0.f;
   f32x4 y = {0.f, 0.f, 0.f, 0.f};
+  Lowered<WINDOW> mine(c);
   auto take = [&](auto n, int i0) {                         // parts i0, i0 + sides, ..., n of them
     constexpr int N = decltype(n)::value;
     f32x4 x[N];
@@ -515,6 +599,12 @@ __global__ __launch_bounds__(32 * kJoinRows) void paged_join_kernel(Attend c, in
     float m = M;
 #pragma unroll
     for (int k = 0; k < N; ++k) m = fmaxf(m, st[k][0]);
+    if constexpr (WINDOW) {
+      uint32_t signs = 0u;
+#pragma unroll
+      for (int k = 0; k < N; ++k) signs |= __float_as_uint(st[k][1]);
+      if (signs >> 31 && !mine.any()) mine.by = c.lower, y = y * mine.by;
+    }
     const float shrink = fast_exp2(M - m);
     M = m;
     L *= shrink;
@@ -522,8 +612,8 @@ __global__ __launch_bounds__(32 * kJoinRows) void paged_join_kernel(Attend c, in
 #pragma unroll
     for (int k = 0; k < N; ++k) {
       const float f = i0 + k * sides < parts ? fast_exp2(st[k][0] - m) : 0.f;
-      L += st[k][1] * f;
-      y += x[k] * f;
+      L += mine.size(st[k][1]) * f;
+      y += x[k] * mine.factor(st[k][1], f);
     }
   };
   if (side < sides) {
@@ -531,20 +621,24 @@ __global__ __launch_bounds__(32 * kJoinRows) void paged_join_kernel(Attend c, in
     for (; i - side + 2 * sides < parts; i += 8 * sides) take(std::integral_constant<int, 8>(), i);
     if (i - side < parts) take(std::integral_constant<int, 2>(), i);
   }
-  if (lane == 0) s_m[row] = M, s_l[row] = L;
+  if (lane == 0) s_m[row] = M, s_l[row] = mine.any() ? -L : L;
   *reinterpret_cast<f32x4*>(&s_y[row][d4]) = y;
   __syncthreads();
   if (row >= heads || (int)blockIdx.y * heads + row >= c.G) return;
   for (int s = 1; s < sides; ++s) M = fmaxf(M, s_m[s * heads + row]);
   L = 0.f;
   y = f32x4{0.f, 0.f, 0.f, 0.f};
+  Lowered<WINDOW> all(c);
+  if constexpr (WINDOW)
+    for (int s = 0; s < sides; ++s)
+      if (__float_as_uint(s_l[s * heads + row]) >> 31) all.by = c.lower;
   for (int s = 0; s < sides; ++s) {
-    const float f = fast_exp2(s_m[s * heads + row] - M);
-    L += s_l[s * heads + row] * f;
-    y += *reinterpret_cast<const f32x4*>(&s_y[s * heads + row][d4]) * f;
+    const float l = s_l[s * heads + row], f = fast_exp2(s_m[s * heads + row] - M);
+    L += all.size(l) * f;
+    y += *reinterpret_cast<const f32x4*>(&s_y[s * heads + row][d4]) * all.factor(l, f);
   }
   const int64_t to = (int64_t)u * c.G + head;
-  put_out(c, to, d4, L != 0.f ? y * (1.f / L) : f32x4{0.f, 0.f, 0.f, 0.f});
+  put_out(c, to, d4, L != 0.f ? all.raise(y * (1.f / L)) : f32x4{0.f, 0.f, 0.f, 0.f});
   if (d4 == 0 && c.lse) c.lse[to] = natural(M, L);
 }
 
