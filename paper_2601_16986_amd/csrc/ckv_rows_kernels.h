@@ -82,12 +82,12 @@ __device__ __forceinline__ const uint8_t* uniform_at(const uint8_t* p) {
 // wait for them, and waits.  They are waited for by hand (arrived()) before the barrier that lets others read.
 __device__ __forceinline__ void load_to_lds(const uint8_t* from, uint32_t to) {
   to = (uint32_t)uniform_i32((int)to);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from) : "memory", "m0");
 }
 __device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t lane_at, uint32_t to) {
   to = (uint32_t)uniform_i32((int)to);
   base = uniform_at(base);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(lane_at), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(lane_at), "s"(base) : "memory", "m0");
 }
 // What lies `more` bytes behind `base`, which is global memory: taken for any memory its load would be waited for as reads of LDS are, by those that follow.
 template <class T>
