@@ -616,6 +616,8 @@ class PagedCache:
                     self.lib.ckv_paged_rows_workspace_bytes(self._ref, seqs._ref, n_picked[0], n_q_heads, at_mask)
             if n == 0:
                 raise CkvError(EINVAL, self.lib.ckv_last_error(None).decode())
+            if len(seqs._workspace) >= 64:               # a server's packed rows may be as many as it has steps
+                seqs._workspace.clear()
             seqs._workspace[key] = n
         if n <= 256:
             return None, None, n
@@ -700,8 +702,8 @@ class PagedCache:
 
     def append_rotated(self, seqs, q, k, v, rotation, *, positions=None, rows=None, first=None, starts=None, out=None):
         """append of keys that a Rotation turns on the way, and of their queries, q bf16 [batch][rows][n_q_heads][128] (or as k and v otherwise): the turned queries, new (uninitialised
-        behind a sequence's last row) or `out`, which may be q.  positions: int32 [batch][rows] ([batch] of single rows, [total] with `starts`), contiguous; by default the rows' positions
-        in their sequences.  q None: keys alone."""
+        behind a sequence's last row) or `out`, which may be q.  positions: int32 [batch][rows] ([batch] of single rows, [total] with `starts`), contiguous: where a row stands
+        in the text (a draft's depth added to the entries before); by default the rows' positions in their sequences.  q None: keys alone."""
         r = self._rows(seqs, k, v, rows, first, starts)
         if rotation.device != self.device:
             raise CkvError(EINVAL, f"a rotation on {rotation.device} with a cache on {self.device}")
