@@ -47,14 +47,20 @@ CKV_PLAN u64_t bits_between(long long e0, long long lo, long long hi) {
 // How a call is cut, by what the host knows: every block of rows has `places` places for pieces, of `least` tiles at least (us with 1, 2, 3, 4, 6 tiles of 64 rows, 13 in all: 17.9, 18.5, 20.3, 21.9, -;
 // of 128 rows, 25 in all: -, 23.4, 22.3, 23.8, 24.0).  Up to four pieces for each compute unit, none where there are as many blocks: a piece beside whole blocks costs its beginning, end and joining for nothing
 // (384 blocks of one length 217 us whole, 234 in pieces), but sequences of many lengths leave units idle without (64 drafts of 32 of them 389 whole, 358 in pieces; one sequence of 131072 4360 and 254).
+// Where that could leave one sequence much longer than the others pieces of more than kLongPiece tiles, and a sequence's blocks do not fill the chip by themselves, every block has one place instead, and the pieces behind it,
+// up to kMorePieces for each compute unit, are dealt out by the lengths on the device (paged_rows_cut_kernel).  us, equal places / dealt out: one sequence of 131072 among others of 200, 8 KV heads with 4 each, 2 x 64 drafts 535 / 345,
+// 32 x 64 1780 / 423, 64 x 64 5190 / 412, 64 x 8 1154 / 166, 600 x 8 3350 / 335, parts of 256 rows of 16 5180 / 1087; 32 x 64 of lengths evenly up to 30000 1250 / 1085.  Of one length: 32 x 64 of 8192 585 / 577, 64 x 8 of 2000 92 / 83,
+// 300 x 8 of 500 152 / 164.  Where it turns, one of n among others of 200: 64 x 64, n = 1500 (47 tiles) 89 / 121, 2000 (63) 108 / 104, 3000 (94) 148 / 131; 300 x 8, n = 4000 (63) 123 / 149, 6000 (94) 174 / 154.
+constexpr int kLongPiece = 80, kMorePieces = 4;
 struct RowsPlan {
   int wide, blocks;              // wavefronts side by side over rows; blocks of rows per unit (sequence, KV head)
   int least, places, workers;    // workers: compute units
   long long pieces;              // workgroups
+  int more;                      // and those for pieces behind their block's places
 };
-CKV_PLAN RowsPlan rows_plan(long long units, int rows, int group, int entries, int n_cu) {
+CKV_PLAN RowsPlan rows_plan(long long units, int rows, int group, int entries, int n_cu, int batch = 1) {
   const long long all = (long long)rows * group;
-  RowsPlan p = {all <= 64 ? 2 : 4, 0, 0, 1, 0, 0};
+  RowsPlan p = {all <= 64 ? 2 : 4, 0, 0, 1, 0, 0, 0};
   const int each = 32 * p.wide, size = rows_tile(p.wide);
   p.blocks = (int)((all + each - 1) / each);
   p.least = p.wide == 4 ? 3 : 1;
@@ -64,6 +70,10 @@ CKV_PLAN RowsPlan rows_plan(long long units, int rows, int group, int entries, i
   p.places = unit_parts(tiles, p.least);
   if (p.places > most) p.places = (int)most;
   if (blocks >= many) p.places = 1;
+  if (batch > 1 && units / batch * p.blocks < n_cu && unit_parts(tiles, p.places) > kLongPiece) {
+    p.places = 1;
+    p.more = kMorePieces * n_cu;
+  }
   p.pieces = units * p.blocks * p.places;
   return p;
 }
@@ -86,6 +96,45 @@ struct RowsCost {
     return 0.75f * (tiles + 11.f * blocks) / workers + 0.5f * longest;
   }
 };
+
+// Tiles of a piece, by the lengths as they are: of the ways to have one, two, four or six pieces for each compute unit, and of no pieces (INT_MAX), the one that ends first.  sum(f): over all
+// blocks of rows, of f(its tiles).  `most` pieces for each compute unit at most; where a block has no more than its places (`only`), the longest has what they leave it.
+template <class Sum>
+CKV_PLAN int rows_cut(const RowsCost& cost, int least, int places, bool only, int most, float longest, const Sum& sum) {
+  const float all = sum([](float tiles) { return tiles; }), blocks = sum([](float) { return 1.f; });
+  float best = cost.whole(blocks, all, longest);
+  int share = 0x7FFFFFFF;
+#if defined(__HIPCC__)
+#pragma unroll 1
+#endif
+  for (int k = 1; k <= most; k += k == 1 ? 1 : 2) {
+    const float pieces_at_most = (float)(k * cost.workers);
+    float s = __builtin_ceilf(all / pieces_at_most);
+    if (s < (float)least) s = (float)least;
+    const float pieces = sum([&](float tiles) { return __builtin_ceilf(tiles / s); });
+    float took = 0.f;
+    if (!only && blocks > pieces_at_most) {          // more blocks than pieces: only the long ones fall into some
+      took = cost.whole(pieces, all, s) + 4.f;
+    } else {
+      if (pieces > pieces_at_most) s = __builtin_ceilf(s * pieces / pieces_at_most);
+      const float left = __builtin_ceilf(longest / (float)places);
+      took = cost.split(k, only && left > s ? left : s);
+    }
+    if (took < best) best = took, share = s < 0x1p30f ? (int)s : 1 << 30;
+  }
+  return share;
+}
+// A block's pieces behind its places, where a sequence's blocks have so many tiles.
+CKV_PLAN int rows_behind(int tiles, int share, int places) {
+  const int parts = unit_parts(tiles, share);
+  return parts > places ? parts - places : 0;
+}
+// Which of a sequence's pieces behind places, `groups` of `blocks` that read the same entries, the index-th is: the blocks of a group, eight apart, go to one part of the chip as long as groups make full rounds.
+CKV_PLAN int rows_behind_piece(int index, int groups, int blocks) {
+  if (index >= groups / 8 * 8 * blocks) return index;
+  const int round = index / (8 * blocks), in = index - round * 8 * blocks;
+  return (round * 8 + in % 8) * blocks + in / 8;
+}
 
 // What a piece's outputs, before they are divided by the sum of weights, may reach without care: kLargeSums times that (more than a block of rows has pieces) is 2^128.
 constexpr float kLargeSum = 0x1p115f, kLargeSums = 0x1p13f;

@@ -60,20 +60,21 @@ bool one_row(const ckv_pages* p, const ckv_seqs* s, int rows, const ckv_mask* m)
 // How a call is cut, and what its pieces leave in the workspace.
 struct RowsSplit {
   RowsPlan plan;
-  size_t partial, ml, parts;    // bytes
-  size_t bytes() const { return partial + ml + parts; }
+  size_t partial, ml, parts, cut;      // bytes
+  size_t bytes() const { return partial + ml + parts + cut; }
 };
 RowsSplit rows_split(const ckv_pages* p, const ckv_seqs* s, int rows, int n_q_heads, const ckv_mask* m, int n_cu) {
   const long long units = (long long)s->batch * p->n_kv_heads;
   const int G = n_q_heads / p->n_kv_heads, most = std::max(std::min(rows, s->max_length), 1);
   const long long spread = m->tree ? most : std::min(most, 128 / G + 2), seen = m->window ? (long long)m->window + m->sinks + spread : s->max_length;
   RowsSplit r{};
-  r.plan = rows_plan(units, most, G, (int)std::min<long long>(seen, s->max_length), n_cu);
-  if (r.plan.places > 1) {
-    const size_t held = (size_t)r.plan.pieces * 32 * r.plan.wide;
+  r.plan = rows_plan(units, most, G, (int)std::min<long long>(seen, s->max_length), n_cu, s->batch);
+  if (r.plan.places > 1 || r.plan.more) {
+    const size_t held = (size_t)(r.plan.pieces + r.plan.more) * 32 * r.plan.wide;
     r.partial = up256(held * kDim * 4);
     r.ml = up256(held * 8);
-    r.parts = up256((size_t)units * r.plan.blocks * 4);
+    r.parts = up256((size_t)units * r.plan.blocks * 8);
+    r.cut = r.plan.more ? up256(((size_t)s->batch + 2) * 4) : 0;
   }
   return r;
 }
@@ -105,7 +106,7 @@ int ckv_paged_attend_rows(const ckv_pages* pages, const ckv_seqs* seqs, const ck
     return attend_one_row(pages, seqs, &query, queries->first, mask, scale_log2e, out, out_dtype, lse, workspace, workspace_bytes, stream);
   }
   const RowsSplit s = rows_split(pages, seqs, queries->rows, queries->n_q_heads, mask, compute_units());
-  const long long units = (long long)seqs->batch * pages->n_kv_heads, grid = rows_grid(units * s.plan.places, (long long)s.plan.blocks);
+  const long long units = (long long)seqs->batch * pages->n_kv_heads, first = rows_grid(units * s.plan.places, (long long)s.plan.blocks), grid = first + s.plan.more;
   if (!launches(grid, kThreads) || !launches(units * s.plan.blocks, 32 * kRowsJoined)) return fail(CKV_EINVAL, "too many rows for one attention (2^24 blocks of 128, a row per query head)");
   if (s.bytes() > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < s.bytes())) return fail(CKV_EWORKSPACE, "workspace too small or misaligned");
   const Paged p = paged_of(pages, seqs);
@@ -126,26 +127,35 @@ int ckv_paged_attend_rows(const ckv_pages* pages, const ckv_seqs* seqs, const ck
   c.least = s.plan.least;
   c.places = s.plan.places;
   c.workers = s.plan.workers;
+  c.more = s.plan.more;
+  c.grid = (int)first;
   c.lower = lowered_by(seqs->max_length);
-  if (s.plan.places > 1) {
+  if (s.bytes() > 0) {
     c.partial = (float*)workspace;
     c.ml = (float*)((char*)workspace + s.partial);
     c.parts = (int32_t*)((char*)workspace + s.partial + s.ml);
+    c.cut = (int32_t*)((char*)workspace + s.partial + s.ml + s.parts);
+  }
+  if (c.more) {
+    auto cut = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(1), dim3(kCutThreads), 0, (hipStream_t)stream, RowsCall{p, c}); };
+    s.plan.wide == 2 ? cut(paged_rows_cut_kernel<2>) : cut(paged_rows_cut_kernel<4>);
+    if (int rc = launched("ckv_paged_attend_rows")) return rc;
   }
   auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), 0, (hipStream_t)stream, RowsCall{p, c}); };
   auto typed = [&](auto e4m3, auto wide) {
     constexpr bool E4M3 = decltype(e4m3)::value;
     constexpr int WIDE = decltype(wide)::value;
-    c.out_bf16 ? launch(paged_rows_kernel<E4M3, WIDE, false>) : launch(paged_rows_kernel<E4M3, WIDE, true>);
+    c.more ? launch(paged_rows_kernel<E4M3, WIDE, true>) : launch(paged_rows_kernel<E4M3, WIDE, false>);
   };
   auto attend = [&](auto wide) { pages->dtype == CKV_E4M3 ? typed(std::true_type(), wide) : typed(std::false_type(), wide); };
   s.plan.wide == 2 ? attend(std::integral_constant<int, 2>()) : attend(std::integral_constant<int, 4>());
   if (int rc = launched("ckv_paged_attend_rows")) return rc;
-  if (s.plan.places == 1) return CKV_OK;
+  if (s.bytes() == 0) return CKV_OK;
   const long long blocks = units * s.plan.blocks, most = 32 * s.plan.wide / kRowsJoined;
   const dim3 joins((unsigned)blocks, (unsigned)std::max(1ll, std::min(most, 8192 / blocks)));
   auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, joins, dim3(32 * kRowsJoined), 0, (hipStream_t)stream, RowsCall{p, c}); };
-  s.plan.wide == 2 ? join(paged_rows_join_kernel<2>) : join(paged_rows_join_kernel<4>);
+  if (c.more) s.plan.wide == 2 ? join(paged_rows_join_kernel<2, true>) : join(paged_rows_join_kernel<4, true>);
+  else s.plan.wide == 2 ? join(paged_rows_join_kernel<2, false>) : join(paged_rows_join_kernel<4, false>);
   return launched("ckv_paged_attend_rows");
 }
 

@@ -21,12 +21,14 @@ struct RowsAttend {
   float* lse;
   float* partial;            // [piece][rows of a block][128]
   float* ml;                 // [piece][rows of a block][2]
-  int32_t* parts;            // [unit][block]: pieces that its blocks fall into
+  int32_t* parts;            // [unit][block][2]: pieces that its blocks fall into, and how far behind the first piece behind any places those behind its own begin
   int64_t tree_seq, tree_row;
   int64_t units;
   float scale_log2e;
   int32_t G, window, sinks, out_bf16;
-  int32_t blocks, least, places, workers;  // RowsPlan
+  int32_t blocks, least, places, workers, more;      // RowsPlan
+  int32_t grid;              // MORE: workgroups before those for pieces behind their block's places
+  int32_t* cut;              // MORE: paged_rows_cut_kernel's
   float lower;               // lowered_by(): what weights are multiplied by where sums would be infinite
 };
 
@@ -121,46 +123,98 @@ __device__ __forceinline__ Told told(const Paged& p, const Rows& r, int b) {
   return {p.lengths[b], first[b], starts[b], starts[r.starts ? b + 1 : b]};
 }
 
-// Tiles of a piece, by the lengths as they are: of the ways to have one, two, four or six pieces for each compute unit, and of no pieces, the one that ends first.  Lanes add up their share of
-// the sequences.
+// Blocks of rows that a sequence has for a KV head, and tiles of its longest.
+struct Have {
+  int blocks, tiles;
+};
+__device__ __forceinline__ Have have_of(const Paged& p, const RowsAttend& c, int block_rows, int size, const Told& t) {
+  const RowSpan s = c.rows.span(t.length, t.first, t.start, t.stop, p.max_length);
+  if (s.count == 0) return Have{0, 0};
+  const int end = s.first + s.count, oldest = c.window ? max(s.first + (c.tree ? 0 : max(s.count - block_rows / c.G, 0)) - c.window, 0) : 0;
+  return Have{(int)(((int64_t)s.count * c.G + block_rows - 1) / block_rows), row_tiles(oldest, end, c.window ? c.sinks : 0, size).count};
+}
+
+// rows_cut by the lengths as they are.  Lanes add up their share of the sequences (mine: the first of them).
 __device__ __forceinline__ int even_share(const Paged& p, const RowsAttend& c, int block_rows, int size, int lane, const Told& mine) {
-  const int per_lane = (p.batch + 63) >> 6, b0 = lane * per_lane;         // mine: sequence b0's
-  struct Have {
-    float blocks, tiles;
-  };
-  auto have = [&](const Told& t) {
-    const RowSpan s = c.rows.span(t.length, t.first, t.start, t.stop, p.max_length);
-    if (s.count == 0) return Have{0.f, 0.f};
-    const int end = s.first + s.count, oldest = c.window ? max(s.first + (c.tree ? 0 : max(s.count - block_rows / c.G, 0)) - c.window, 0) : 0;
-    return Have{(float)(((int64_t)s.count * c.G + block_rows - 1) / block_rows), (float)row_tiles(oldest, end, c.window ? c.sinks : 0, size).count};
-  };
-  Have one = {0.f, 0.f};
-  if (b0 < p.batch) one = have(mine);
-  auto each = [&](auto count) {                    // sum over the sequences' blocks of rows
-    float sum = one.blocks * count(one.tiles);
+  const int per_lane = (p.batch + 63) >> 6, b0 = lane * per_lane;
+  Have one = {0, 0};
+  if (b0 < p.batch) one = have_of(p, c, block_rows, size, mine);
+  auto sum = [&](auto count) {                     // over the sequences' blocks of rows
+    float all = (float)one.blocks * count((float)one.tiles);
     for (int b = b0 + 1; b < b0 + per_lane && b < p.batch; ++b) {
-      const Have more = have(told(p, c.rows, b));
-      sum += more.blocks * count(more.tiles);
+      const Have more = have_of(p, c, block_rows, size, told(p, c.rows, b));
+      all += (float)more.blocks * count((float)more.tiles);
     }
-    return wave_sum_f32(sum) * p.hkv;
+    return wave_sum_f32(all) * p.hkv;
   };
-  float longest = one.tiles;
-  for (int b = b0 + 1; b < b0 + per_lane && b < p.batch; ++b) longest = fmaxf(longest, have(told(p, c.rows, b)).tiles);
+  float longest = (float)one.tiles;
+  for (int b = b0 + 1; b < b0 + per_lane && b < p.batch; ++b) longest = fmaxf(longest, (float)have_of(p, c, block_rows, size, told(p, c.rows, b)).tiles);
   longest = __uint_as_float(~wave_min_u32(~__float_as_uint(longest)));
-  const float all = each([](float tiles) { return tiles; }), blocks = each([](float) { return 1.f; });
   const RowsCost cost = {block_rows, c.workers};
-  float best = cost.whole(blocks, all, longest);
-  int share = INT32_MAX;
-#pragma unroll 1
-  for (int k = 1; k <= 6; k += k == 1 ? 1 : 2) {
-    const float most = (float)(k * c.workers);
-    float s = fmaxf(ceilf(all / most), (float)c.least);
-    const float pieces = each([&](float tiles) { return ceilf(tiles / s); });
-    if (pieces > most) s = ceilf(s * pieces / most);
-    const float took = cost.split(k, s);
-    if (took < best) best = took, share = (int)s;
+  return rows_cut(cost, c.least, c.places, true, 6, longest, sum);
+}
+
+// The same, once for a call whose blocks may have more pieces than places: cut[0] = tiles of a piece, cut[1 + b] = pieces behind their blocks' places of the sequences before b, numbered by sequence,
+// KV head, block and piece; cut[1 + batch] all of them.  One workgroup, its threads adding up sequences side by side; three trips to memory and a dozen sums over the workgroup.  (Every workgroup of the attention for itself, as
+// without such pieces: 300 sequences of 8 drafts over 500 entries 242 us where they now take 164.)
+constexpr int kCutThreads = 512;
+template <int WIDE>
+__global__ __launch_bounds__(kCutThreads) void paged_rows_cut_kernel(RowsCall call) {
+  const Paged& p = call.p;
+  const RowsAttend& c = call.c;
+  constexpr int kRows = 32 * WIDE, kUnit = 32 * (kAttendWaves / WIDE), kWaves = kCutThreads / 64;
+  __shared__ float s_sum[2][kWaves];
+  __shared__ int s_upto[kWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  auto have = [&](int b) { return have_of(p, c, kRows, kUnit, told(p, c.rows, b)); };
+  Have one = {0, 0};
+  if (tid < p.batch) one = have(tid);
+  int turn = 0;
+  auto over = [&](float mine, auto of_wave, auto op) {
+    mine = of_wave(mine);
+    turn ^= 1;                                     // (the sums of the one before may still be read)
+    if (lane == 0) s_sum[turn][wave] = mine;
+    __syncthreads();
+    float all = s_sum[turn][0];
+    for (int w = 1; w < kWaves; ++w) all = op(all, s_sum[turn][w]);
+    return all;
+  };
+  auto sum = [&](auto count) {
+    float all = (float)one.blocks * count((float)one.tiles);
+    for (int b = tid + kCutThreads; b < p.batch; b += kCutThreads) {
+      const Have more = have(b);
+      all += (float)more.blocks * count((float)more.tiles);
+    }
+    return over(all, [](float x) { return wave_sum_f32(x); }, [](float x, float y) { return x + y; }) * p.hkv;
+  };
+  float longest = (float)one.tiles;
+  for (int b = tid + kCutThreads; b < p.batch; b += kCutThreads) longest = fmaxf(longest, (float)have(b).tiles);
+  longest = over(longest, [](float x) { return __uint_as_float(~wave_min_u32(~__float_as_uint(x))); }, [](float x, float y) { return fmaxf(x, y); });
+  const RowsCost cost = {kRows, c.workers};
+  int share = rows_cut(cost, c.least, c.places, false, kMorePieces, longest, sum);
+  // never more than there are workgroups for: by floats so that they can be counted, then as they are
+  const float behind = sum([&](float tiles) { return (float)rows_behind((int)tiles, share, c.places); });
+  if (!(behind <= 2.f * (float)c.more)) share = INT32_MAX;
+  for (;;) {
+    int begun = 0;
+    for (int b0 = 0; b0 < p.batch; b0 += kCutThreads) {
+      const int b = b0 + tid;
+      const Have mine = b0 == 0 ? one : b < p.batch ? have(b) : Have{0, 0};
+      const int own = p.hkv * mine.blocks * rows_behind(mine.tiles, share, c.places), upto = wave_scan_i32(own, lane);
+      if (lane == 63) s_upto[wave] = upto;
+      __syncthreads();
+      int before = begun;
+      for (int w = 0; w < kWaves; ++w) {
+        before += w < wave ? s_upto[w] : 0;
+        begun += s_upto[w];
+      }
+      if (b < p.batch) c.cut[1 + b] = before + upto - own;
+      __syncthreads();
+    }
+    if (tid == 0) c.cut[0] = share, c.cut[1 + p.batch] = begun;
+    if (begun <= c.more) return;
+    share = INT32_MAX;
   }
-  return share;
 }
 
 // One workgroup of four wavefronts per piece: 32 WIDE rows (row = one query head of one of the call's rows of a sequence, heads of a KV head side by side) over some tiles
@@ -184,7 +238,7 @@ __device__ __forceinline__ int even_share(const Paged& p, const RowsAttend& c, i
 // Built, measured and not kept: a step's loads between its products (25 drafts in a window of 1024 55 us instead of 52, prompts no faster), a higher priority for wavefronts that load (the same), 32 rows a workgroup with
 // 128 entries at once (128 KB of LDS: 8 bits 108 us for 8 rows of 4 heads over 4096 entries of 32 sequences where blocks of 64 rows with idle wavefronts take 83; bf16 113 and 118), 8 bits written to LDS
 // in another order of rows, the next logits a turn early with their largest value beside the last outputs (both the same).
-template <bool E4M3, int WIDE, bool F32>
+template <bool E4M3, int WIDE, bool MORE>
 __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) {
   const Paged& p = call.p;
   const RowsAttend& c = call.c;
@@ -198,14 +252,48 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i32(tid >> 6), j = lane & 31, half = lane >> 5, wq = wave % WIDE, wk = wave / WIDE;
   if (tid == 0) s_odd = s_far = 0;
-  const uint32_t each = (uint32_t)c.blocks, piece = rows_piece(blockIdx.x, (uint32_t)c.units * (uint32_t)c.places, each);
-  if (piece == ~0u) return;
-  const uint32_t group = (uint32_t)uniform_i32((int)(piece / each));
-  const RowsGroup of = rows_group(group, (uint32_t)c.units);
-  const int part = uniform_i32((int)of.part), u = uniform_i32((int)of.unit), blk = uniform_i32((int)(each - 1 - (piece - group * each)));       // the last rows have the most to do
-  const int b = uniform_i32((int)((uint32_t)u / (uint32_t)p.hkv)), h = u - b * p.hkv;
+  const uint32_t each = (uint32_t)c.blocks;
+  int part, b, h, blk, at_behind = 0, share = 0, limit = c.places, begins = 0;      // MORE: tiles of a piece; the most that the block can fall into; where its pieces behind its places begin
+  const bool behind = MORE && blockIdx.x >= (uint32_t)c.grid;
+  if constexpr (MORE) share = uniform_i32(c.cut[0]);
+  if (behind) {
+    int index = (int)(blockIdx.x - (uint32_t)c.grid), above = p.batch;
+    if (index >= uniform_i32(c.cut[1 + p.batch])) return;
+    for (b = 0; above - b > 1;) {                  // the last sequence that begins at it or before it, 64 at a time
+      const int step = (above - b + 63) >> 6, at = b + lane * step;
+      const u64 upto = __ballot(at < above && c.cut[1 + min(at, above - 1)] <= index);
+      b += step * (63 - __clzll((long long)upto));
+      above = min(above, b + step);
+    }
+    index -= uniform_i32(c.cut[1 + b]);
+    const Have of = have_of(p, c, kRows, kUnit, told(p, c.rows, b));
+    const int blocks = uniform_i32(of.blocks), more = rows_behind(uniform_i32(of.tiles), share, c.places);
+    const int piece = rows_behind_piece(index, p.hkv * more, blocks), group = piece / blocks;
+    blk = blocks - 1 - (piece - group * blocks);
+    part = group / p.hkv;
+    h = group - part * p.hkv;
+    // where the block's are kept, whatever the order in which they are taken
+    at_behind = (h * blocks + blk) * more + part + uniform_i32(c.cut[1 + b]);
+    part += c.places;
+  } else {
+    const uint32_t piece = rows_piece(blockIdx.x, (uint32_t)c.units * (uint32_t)c.places, each);
+    if (piece == ~0u) return;
+    const uint32_t group = (uint32_t)uniform_i32((int)(piece / each));
+    const RowsGroup of = rows_group(group, (uint32_t)c.units);
+    part = uniform_i32((int)of.part), blk = uniform_i32((int)(each - 1 - (piece - group * each)));       // the last rows have the most to do
+    b = uniform_i32((int)(of.unit / (uint32_t)p.hkv)), h = uniform_i32((int)of.unit) - b * p.hkv;
+  }
+  part = uniform_i32(part), b = uniform_i32(b), h = uniform_i32(h), blk = uniform_i32(blk);
+  if constexpr (MORE) at_behind = uniform_i32(at_behind);
+  const int u = b * p.hkv + h;
   const int64_t block_index = (int64_t)u * c.blocks + blk;
-  const Told own = told(p, c.rows, b), mine = told(p, c.rows, min(lane * ((p.batch + 63) >> 6), p.batch - 1));
+  const Told own = told(p, c.rows, b), mine = told(p, c.rows, MORE ? b : min(lane * ((p.batch + 63) >> 6), p.batch - 1));
+  if constexpr (MORE) {
+    const Have of = have_of(p, c, kRows, kUnit, own);
+    const int more = rows_behind(uniform_i32(of.tiles), share, c.places);
+    limit += more;
+    begins = uniform_i32(c.cut[1 + b]) + (h * uniform_i32(of.blocks) + blk) * more;
+  }
   int bad = p.max_length < own.length || own.length < 0 ? PAGED_BAD_LENGTH : 0;
   const RowSpan span = c.rows.span(uniform_i32(own.length), uniform_i32(own.first), uniform_i32(own.start), uniform_i32(own.stop), p.max_length);
   const int64_t q_base = c.rows.starts ? uniform_i32(own.start) * c.rows.row_stride : b * c.rows.seq_stride;
@@ -213,7 +301,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
   const uint32_t r0 = (uint32_t)blk * kRows, n_rows = (uint32_t)uniform_i32(span.count) * (uint32_t)c.G;
   if (r0 >= n_rows) {
     if (part == 0 && tid == 0) {
-      if (c.parts) c.parts[block_index] = 0;
+      if (c.parts) c.parts[2 * block_index] = 0;
       if (blk == 0) p.report(bad);
     }
     return;
@@ -271,10 +359,14 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
 
   RowTiles tiles = row_tiles(oldest, end, sinks, kUnit);
   tiles = {uniform_i32(tiles.sinks), uniform_i32(tiles.base), uniform_i32(tiles.count)};
-  int share = tiles.count;
-  if (c.places > 1) share = rows_share(tiles.count, even_share(p, c, kRows, kUnit, lane, mine), c.places);
-  const int parts = uniform_i32(unit_parts(tiles.count, share));
-  if (part == 0 && tid == 0 && c.parts) c.parts[block_index] = parts;
+  int each_part = tiles.count;
+  if constexpr (MORE) each_part = rows_share(tiles.count, share, limit);
+  else if (c.places > 1) each_part = rows_share(tiles.count, even_share(p, c, kRows, kUnit, lane, mine), c.places);
+  const int parts = uniform_i32(unit_parts(tiles.count, each_part));
+  if (part == 0 && tid == 0 && c.parts) {
+    c.parts[2 * block_index] = parts;
+    if constexpr (MORE) c.parts[2 * block_index + 1] = begins;
+  }
   if (part >= parts) return;
   const int n_first = uniform_i32(part_begin(tiles.count, parts, part)), n_last = uniform_i32(part_begin(tiles.count, parts, part + 1));
 
@@ -723,7 +815,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
   const int64_t out_row = a->c.rows.starts ? a->c.rows.starts[b] : (int64_t)b * a->c.rows.rows;
   float *lse = a->c.lse, *partial = a->c.partial, *ml = a->c.ml;
   uint8_t* out = a->c.out;
-  const int places = a->c.places;
+  const bool out_bf16 = a->c.out_bf16;
+  const int64_t piece = behind ? a->c.units * a->c.blocks * a->c.places + at_behind : block_index * a->c.places + part;
   const float raised = 1.f / lowered;
   constexpr int kEnd = 4;                          // rows at once
   const int chunk = tid & 31;
@@ -749,13 +842,13 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
       const int r = r_first + kThreads / 32 * i;
       if (r0 + r >= n_rows) break;
       if (parts > 1) {
-        const int64_t at = (block_index * places + part) * kRows + r;
+        const int64_t at = piece * kRows + r;
         *reinterpret_cast<f32x4*>(partial + at * kDim + 4 * chunk) = y[i];
         if (chunk == 0) *reinterpret_cast<f32x2*>(ml + 2 * at) = f32x2{M[i], lowered < 1.f ? -L[i] : L[i]};
       } else {
         const int t = (int)((r0 + r) / G);
         const int64_t to = (out_row + t) * (G * hkv) + h * G + (int)(r0 + r - (uint32_t)t * G);
-        put_row(out, !F32, to, 4 * chunk, L[i] != 0.f ? y[i] * (1.f / L[i]) * raised : f32x4{0.f, 0.f, 0.f, 0.f});
+        put_row(out, out_bf16, to, 4 * chunk, L[i] != 0.f ? y[i] * (1.f / L[i]) * raised : f32x4{0.f, 0.f, 0.f, 0.f});
         if (chunk == 0 && lse) lse[to] = natural(M[i], L[i]);
       }
     }
@@ -766,14 +859,15 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
 // Joins the pieces of blocks of rows that have several: 32 threads a row, four dimensions each, eight rows a workgroup, which takes every `gridDim.y`-th eight of a block (64 drafts of 32
 // sequences of many lengths, 512 blocks: 14.6 us with all of a block's eights side by side, 19.4 with four).  Bound by trips: parts, lengths, partial outputs, eight of them at once.
 constexpr int kRowsJoined = 8;
-template <int WIDE>
+template <int WIDE, bool MORE>
 __global__ __launch_bounds__(32 * kRowsJoined) void paged_rows_join_kernel(RowsCall call) {
   const Paged& p = call.p;
   const RowsAttend& c = call.c;
   constexpr int kRows = 32 * WIDE;
   const int64_t block_index = blockIdx.x;
-  const int parts = c.parts[block_index];
+  const int parts = c.parts[2 * block_index];
   if (parts <= 1) return;
+  const int64_t begins = block_index * c.places, behind = MORE ? c.units * c.blocks * c.places + c.parts[2 * block_index + 1] - c.places : 0;
   const int u = (int)(block_index / c.blocks), blk = (int)(block_index - (int64_t)u * c.blocks), b = u / p.hkv, h = u - b * p.hkv;
   int64_t base;
   const RowSpan span = c.rows.span(b, p.lengths[b], p.max_length, base);
@@ -789,7 +883,8 @@ __global__ __launch_bounds__(32 * kRowsJoined) void paged_rows_join_kernel(RowsC
       f32x4 x[N];
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int64_t at = (block_index * c.places + min(i0 + i, parts - 1)) * kRows + in;
+        const int part = min(i0 + i, parts - 1);
+        const int64_t at = ((!MORE || part < c.places ? begins : behind) + part) * kRows + in;
         st[i] = *reinterpret_cast<const f32x2*>(c.ml + 2 * at);
         x[i] = *reinterpret_cast<const f32x4*>(c.partial + at * kDim + d4);
       }
