@@ -223,7 +223,7 @@ __global__ __launch_bounds__(kCutThreads) void paged_rows_cut_kernel(RowsCall ca
 //   outputs  V^T P^T with the logits' registers as operand, entries in the order in which K Q^T leaves them, and values read out of LDS transposed (columns = rows again,
 //            so that what shrinks them is the lane's own too).
 // Weights go in as three bf16 terms, which hold the 24 bits of a float: 32 products for 32 entries where one term would need 16.  (Two terms, 16 bits, take a fifth less time, prompts below 1.44 ms and drafts 245 us where
-// three take 1.79 and 290, and leave outputs that nearly cancel off by 2^-18 of their terms: of 8388608 bf16 outputs over up to 9350 entries 20920 then round the other way than the exact ones, 3102 with three
+// three take 1.79 and 290, and leave outputs that nearly cancel off by up to 2^-17 of their terms: of 8388608 bf16 outputs over up to 9350 entries 20920 then round the other way than the exact ones, 3102 with three
 // terms, 7017 in float arithmetic throughout.)  An entry that only some rows of the block see gives the others
 // nothing, whatever its value: where something that is not finite comes out the piece is done again with the finite values alone, and rows that give others weight
 // get NaN where those are.  Where finite values add up to 2^115 it is done once more with lowered weights (lowered_by), whose sums stay finite; the sum of weights, which is not lowered, then has a sign
