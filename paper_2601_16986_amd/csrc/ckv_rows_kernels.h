@@ -67,6 +67,7 @@ __device__ __forceinline__ void apart() { asm volatile(""); }
 // What is worked out here is not put off until it is used.
 template <class T>
 __device__ __forceinline__ void here(T& x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void here_scalar(int& x) { asm volatile("" : "+s"(x)); }
 // Nothing moves from one side to the other.
 __device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
 
@@ -227,7 +228,9 @@ __global__ __launch_bounds__(kCutThreads) void paged_rows_cut_kernel(RowsCall ca
 // terms, 7017 in float arithmetic throughout.)  An entry that only some rows of the block see gives the others
 // nothing, whatever its value: where something that is not finite comes out the piece is done again with the finite values alone, and rows that give others weight
 // get NaN where those are.  Where finite values add up to 2^115 it is done once more with lowered weights (lowered_by), whose sums stay finite; the sum of weights, which is not lowered, then has a sign
-// for the join.  (What only these ways need is what the variants of 8 bits keep in scratch, 16 and 8 registers: written before the first tile, read where a piece is done again.)
+// for the join.  No vector register goes to scratch; 67 to
+// 98 scalar ones lie in lanes of vector registers, moved there once (104 to 138, and with 8 bits 16 vector registers in scratch, where the ways that a piece is done again held what they need from the beginning on: 8 drafts of 4
+// short sequences 22.4 us, now 21.4).
 // What bounds it: long pieces of many rows by what moves, in LDS's time and in power: each wavefront reads all keys and values out of LDS for its 32 rows, 16 KB for the 24 products of 32 entries, beside the
 // entries that come in.  A copy that reads nothing out of LDS takes 18 % less, one that loads no entries 18 % less, one without both 28 % (at a higher clock, too), which is what the products take; reads
 // asked for a turn earlier change nothing, so it is not their latency; the exponentials and splitting of weights fit between
@@ -316,7 +319,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
   for (int s = 0; s < 8; ++s) q[s] = __builtin_bit_cast(bf16x8, load16(c.rows.k + q_base + token * c.rows.row_stride + (h * c.G + g) * c.rows.head_stride + 2 * (16 * s + 8 * half)));
 
   // ---- which entries the lane's row sees: lo .. hi - 1, the first `sinks`, and of the call's rows those in s_see
-  const int sinks = c.window ? c.sinks : 0;
+  int sinks = c.window ? c.sinks : 0;
   int position = first + token, hi = position + 1, oldest, end = first + t_hi + 1;
   if (c.tree) {
     const int words = (count + 63) >> 6;
@@ -368,14 +371,15 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
     if constexpr (MORE) c.parts[2 * block_index + 1] = begins;
   }
   if (part >= parts) return;
-  const int n_first = uniform_i32(part_begin(tiles.count, parts, part)), n_last = uniform_i32(part_begin(tiles.count, parts, part + 1));
+  int n_first = uniform_i32(part_begin(tiles.count, parts, part));
+  const int n_last = uniform_i32(part_begin(tiles.count, parts, part + 1));
 
   f32x16 acc[4];
   float m_run, l_run;
   const float scale_log2e = c.scale_log2e;
 
   // ---- units' way into LDS: rows of 256 bytes, bf16 straight there, 8 bits through registers
-  const int units = n_last - n_first;
+  int units = n_last - n_first;
   auto unit_at = [&](int i) CKV_INLINE { return tiles.tile(n_first + i) * kUnit; };
   auto seen = [&](int e) CKV_INLINE { return (bool)((e < end) & ((e >= oldest) | (e < sinks))); };
   // Where kPageSlots pages lie, a lane each, of the sequence's pages kPageSlots * window and on, and the ones before them (the pool's first instead of one that is not there).
@@ -388,12 +392,15 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
   constexpr int kOnce = E4M3 ? 32 : 16;          // rows of a load
   constexpr int kMine = kOnce / kAttendWaves;     // of them a wavefront's, always in one page
   const int r_in = tid / (kThreads / kOnce);     // the thread's
-  const int shift = p.shift, page_mask = p.page_size() - 1, slot_stride = p.slot_stride;
-  const uint32_t in_row = 16 * (E4M3 ? tid & 7 : (tid & 15) ^ swizzle(r_in)), lane_at = (uint32_t)(r_in * slot_stride) + in_row, next_at = lane_at + (uint32_t)(kOnce * slot_stride), wave_at = (uint32_t)(kMine * wave * slot_stride), near_at = lane_at - wave_at;
-  const uint32_t scale_near = (uint32_t)(2 * (r_in - kMine * wave));
+  int shift = p.shift, page_mask = p.page_size() - 1, slot_stride = p.slot_stride;
+  const uint32_t in_row = 16 * (E4M3 ? tid & 7 : (tid & 15) ^ swizzle(r_in)), lane_at = (uint32_t)(r_in * slot_stride) + in_row, next_at = lane_at + (uint32_t)(kOnce * slot_stride), wave_at = (uint32_t)(kMine * wave * slot_stride);
+  uint32_t near_at = lane_at - wave_at;
+  uint32_t scale_near = (uint32_t)(2 * (r_in - kMine * wave));
   const u64 k_to_v = (u64)p.v - (u64)p.k;
-  auto pages = [&](int logical, Known& to) CKV_INLINE {
+  auto pages = [&](int w, Known& to) CKV_INLINE {
     const auto a = args();
+    int logical = w * kPageSlots + lane;
+    here(logical);                               // (as at the careful pieces)
     const int64_t from = (int64_t)logical << shift, upto = from + page_mask + 1;
     const bool needed = logical < a->p.columns && from < end && (upto > oldest || from < sinks);
     const int page = needed ? a->p.table[(int64_t)b * a->p.table_stride + logical] : -1;
@@ -460,7 +467,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
           if (w != known.window) {
             before = known;
             known.window = w;
-            pages(w * kPageSlots + lane, known);
+            pages(w, known);
           }
           from = known;
           if (!all) plain = uniform_i32(unit + 1);
@@ -471,7 +478,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
         } else {
           from.row = w == known.window ? known.row : before.row;
           from.scale = w == known.window ? known.scale : before.scale;
-          if (w != known.window && w != before.window) pages(w * kPageSlots + lane, from);
+          if (w != known.window && w != before.window) pages(w, from);
         }
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
@@ -773,7 +780,9 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
   if (!(fabsf(nothing) < INFINITY)) s_odd = 1;
   __syncthreads();
   if (uniform_i32(s_odd)) {
-    apart();
+    // (what is worked out of these again would otherwise wait from the beginning on, in lanes of vector registers and in scratch)
+    here(near_at), here(scale_near);
+    for (int* x : {&tiles.sinks, &tiles.base, &end, &oldest, &sinks, &units, &n_first, &shift, &page_mask, &slot_stride}) here_scalar(*x);
 #pragma unroll 1
     for (int turn = 0; turn < 2; ++turn) {
       if (turn == 1) {
