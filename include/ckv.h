@@ -514,7 +514,7 @@ size_t ckv_paged_rows_workspace_bytes(const ckv_pages* pages, const ckv_seqs* se
  * zeros and -inf.  Logits, statistics and sums are held in float, weights in its 24 bits.  Entries that a row does not see do not change its outputs, whatever
  * they hold; one that it sees and gives weight must be finite (NaN comes out otherwise, in those dimensions; a weight that is nothing in float beside
  * the row's largest may count either way).  Finite values may be as large as they come: where a
- * block's sums would reach 2^115 before they are divided, weights below 2^-86 of a row's largest count as nothing.  Table entries of pages that no row of the call sees are not looked at: pages that have left
+ * block's sums reach 2^115 before they are divided, or are no number, weights below 2^-86 of a row's largest count as nothing.  Table entries of pages that no row of the call sees are not looked at: pages that have left
  * every window can be given to other sequences.  A sequence's rows times query heads per KV head: below 2^31.  workspace: 256-byte aligned, NULL where 256 are needed. */
 int ckv_paged_attend_rows(const ckv_pages* pages, const ckv_seqs* seqs, const ckv_row_queries* queries, const ckv_mask* mask, float softmax_scale, void* out,
                           int32_t out_dtype, float* lse, void* workspace, size_t workspace_bytes, void* stream);

@@ -490,24 +490,22 @@ __global__ __launch_bounds__(kThreads) void paged_attend_kernel(Paged p, Attend 
   };
   blocks(std::false_type());
   if constexpr (WINDOW) {
-    // With care where something that is no number came out, so that values reach those heads only that give them weight; then with lowered weights too where
-    // finite values add up to so much that pieces' sums might be infinite.
-    float nothing = 0.f;
+    // With care where something that is no number came out, so that values reach those heads only that give them weight; then with lowered weights too where that
+    // leaves anything so large that pieces' sums might be infinite, or no number.
+    auto sound = [&]() __attribute__((always_inline)) {        // below 2^115, and numbers
+      float nothing = 0.f;
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt)
+      for (int dt = 0; dt < 8; ++dt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) nothing = fmaf(acc[dt][i], kLargeSums, nothing);
-    if (__any(!(fabsf(nothing) < INFINITY))) {
+        for (int i = 0; i < 4; ++i) nothing = fmaf(acc[dt][i], kLargeSums, nothing);
+      return fabsf(nothing) < INFINITY;
+    };
+    if (__any(!sound())) {
       asm volatile("");                                    // keeps this in the branch
 #pragma unroll 1
       for (int turn = 0; turn < 2; ++turn) {
         if (turn == 1) {
-          float most = 0.f;
-#pragma unroll
-          for (int dt = 0; dt < 8; ++dt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(acc[dt][i]));
-          if (!__any(most >= kLargeSum)) break;
+          if (!__any(!sound())) break;                     // (what is no number may be infinity less infinity)
           lowered = c.lower;
         }
 #pragma unroll

@@ -770,14 +770,17 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
     put(buf ^ 1);
   }
   __syncthreads();
-  // Once more with care where a page was missing, or something that is no number came out: a value that only some rows see must not reach the others.  And once more with lowered weights where finite
-  // values, of up to 2^128, add up to so much that a few thousand pieces' sums might be infinite.
-  float nothing = 0.f;
+  // Once more with care where a page was missing, or something that is no number came out: a value that only some rows see must not reach the others.  And once more with lowered weights where that leaves
+  // anything so large that a few thousand pieces' sums might be infinite (finite values are below 2^128), or no number, as infinite sums of both signs do.
+  auto sound = [&]() CKV_INLINE {                // below 2^115, and numbers
+    float nothing = 0.f;
 #pragma unroll
-  for (int d = 0; d < 4; ++d)
+    for (int d = 0; d < 4; ++d)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) nothing = fmaf(acc[d][i], kLargeSums, nothing);
-  if (!(fabsf(nothing) < INFINITY)) s_odd = 1;
+      for (int i = 0; i < 16; ++i) nothing = fmaf(acc[d][i], kLargeSums, nothing);
+    return fabsf(nothing) < INFINITY;
+  };
+  if (!sound()) s_odd = 1;
   __syncthreads();
   if (uniform_i32(s_odd)) {
     // (what is worked out of these again would otherwise wait from the beginning on, in lanes of vector registers and in scratch)
@@ -786,12 +789,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(RowsCall call) 
 #pragma unroll 1
     for (int turn = 0; turn < 2; ++turn) {
       if (turn == 1) {
-        float most = 0.f;
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(acc[d][i]));
-        if (most >= kLargeSum) s_far = 1;
+        if (!sound()) s_far = 1;                 // (what is no number may be infinity less infinity)
         __syncthreads();
         if (!uniform_i32(s_far)) break;
         lowered = args()->c.lower;

@@ -15,12 +15,12 @@ def ints(x):
     return torch.as_tensor(np.asarray(x, np.int32)).to(DEV)
 
 
-def filled(lengths, hkv, ps, e4m3, seed, large):
-    """Values between LARGE / 2 and LARGE, all of one sign, in the entries of which `large` (a function of positions) holds; of size 1 in the others."""
+def filled(lengths, hkv, ps, e4m3, seed, large, signs=(1.0,)):
+    """Values between LARGE / 2 and LARGE, of these signs, in the entries of which `large` (a function of positions) holds; of size 1 in the others."""
     def make(rng, shape):
         k, v = bf16(rng.standard_normal(shape)), bf16(rng.standard_normal(shape))
         at = np.broadcast_to(large(np.arange(shape[1]))[None, :, None, None], shape)
-        return k, np.where(at, bf16(rng.uniform(0.5, 1.0, shape) * LARGE), v)
+        return k, np.where(at, bf16(rng.uniform(0.5, 1.0, shape) * rng.choice(signs, shape) * LARGE), v)
 
     return Filled(lengths, hkv, ps, e4m3, seed=seed, make=make)
 
@@ -44,6 +44,54 @@ def test_large_values(e4m3, f32, rows, hq, packed, which):
     else:
         out, lse = f.cache.attend_rows(f.seqs, x, f32=f32, lse=True)
     check_rows(f, q, out, [rows] * 3, lse=lse)
+
+
+@pytest.mark.parametrize("e4m3", [True, False])
+@pytest.mark.parametrize("rows,hq", [(1, 8), (3, 4), (9, 10), (70, 6)])
+@pytest.mark.parametrize("packed", [False, True])
+def test_large_values_of_both_signs(e4m3, rows, hq, packed):
+    """Sums that would be infinite one way and the other, which is no number; logits that rise from tile to tile so that weights above 1 meet them."""
+    lengths = [900, 75]
+    f = filled(lengths, 2, 64, e4m3, rows, lambda e: e % 3 > 0, signs=(-1.0, 1.0))
+    keys, values = f.rows
+    keys[..., 0] = bf16(np.arange(900) / 16)[None, :, None]
+    f.cache.append(f.seqs, *(torch.from_numpy(x).to(DEV).bfloat16() for x in (keys, values)))
+    f.k = [[f.held(keys[b, :n, h]) for h in range(2)] for b, n in enumerate(lengths)]
+    q = bf16(f.rng.standard_normal((2, rows, hq, 128)))
+    q[..., 0] = 4.0
+    if packed:
+        out, lse = f.cache.attend_rows(f.seqs, device(q).view(2 * rows, hq, 128), rows=rows, starts=ints(np.arange(3) * rows), f32=True, lse=True)
+        out, lse = out.view(q.shape), lse.view(q.shape[:3])
+    else:
+        out, lse = f.cache.attend_rows(f.seqs, device(q), f32=True, lse=True)
+    assert torch.isfinite(out).all()
+    check_rows(f, q, out, [rows] * 2, lse=lse)
+
+
+@pytest.mark.parametrize("e4m3", [True, False])
+@pytest.mark.parametrize("rows,hq", [(1, 8), (3, 4), (70, 6)])
+@pytest.mark.parametrize("packed", [False, True])
+def test_sums_that_are_no_number_and_nowhere_large(e4m3, rows, hq, packed):
+    """One dimension alone, large and positive in the first tiles, large and negative, with weights of 2^7 relative to those, in the later ones: what it would add up to is infinity less infinity, in no
+    other place anything is large.  So many sequences (all of the same pages) that none is cut."""
+    batch = 700
+    f = Filled([256 + rows], 2, 64, e4m3, seed=rows)
+    keys, values = f.rows
+    keys[0, :128, :, 0], keys[0, 128:256, :, 0], keys[0, 256:, :, 0] = 0.0, 5.0, -5.0
+    values[0, :128, :, 7], values[0, 128:256, :, 7] = LARGE, -LARGE
+    f.cache.append(f.seqs, *(torch.from_numpy(x).to(DEV).bfloat16() for x in f.rows))
+    f.k, f.v = ([[f.held(x[0, :, h]) for h in range(2)]] for x in (keys, values))
+    seqs = f.cache.sequences(torch.from_numpy(f.table[[0] * batch]).to(DEV), torch.full((batch,), f.lengths[0], dtype=torch.int32, device=DEV))
+    q = bf16(f.rng.standard_normal((1, rows, hq, 128)) / 16)
+    q[..., 0] = 1.0
+    x = device(q).expand(batch, rows, hq, 128).contiguous()
+    if packed:
+        out, lse = f.cache.attend_rows(seqs, x.view(batch * rows, hq, 128), rows=rows, starts=ints(np.arange(batch + 1) * rows), scale=1.0, f32=True, lse=True)
+        out, lse = out.view(x.shape), lse.view(x.shape[:3])
+    else:
+        out, lse = f.cache.attend_rows(seqs, x, scale=1.0, f32=True, lse=True)
+    assert torch.isfinite(out).all() and torch.equal(out[0], out[699])
+    check_rows(f, q, out[:1], [rows], lse=lse[:1], scale=1.0)
 
 
 @pytest.mark.parametrize("e4m3", [True, False])
