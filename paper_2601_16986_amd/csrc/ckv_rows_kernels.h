@@ -168,8 +168,15 @@ __global__ __launch_bounds__(kCutThreads) void paged_rows_cut_kernel(RowsCall ca
   __shared__ int s_upto[kWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   auto have = [&](int b) { return have_of(p, c, kRows, kUnit, told(p, c.rows, b)); };
-  Have one = {0, 0};
-  if (tid < p.batch) one = have(tid);
+  constexpr int kHeld = 4;                         // of a thread's sequences in registers
+  Have held[kHeld];
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) held[i] = tid + i * kCutThreads < p.batch ? have(tid + i * kCutThreads) : Have{0, 0};
+  auto each = [&](auto what) {                     // of the thread's sequences
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) what(held[i]);
+    for (int b = tid + kHeld * kCutThreads; b < p.batch; b += kCutThreads) what(have(b));
+  };
   int turn = 0;
   auto over = [&](float mine, auto of_wave, auto op) {
     mine = of_wave(mine);
@@ -181,15 +188,12 @@ __global__ __launch_bounds__(kCutThreads) void paged_rows_cut_kernel(RowsCall ca
     return all;
   };
   auto sum = [&](auto count) {
-    float all = (float)one.blocks * count((float)one.tiles);
-    for (int b = tid + kCutThreads; b < p.batch; b += kCutThreads) {
-      const Have more = have(b);
-      all += (float)more.blocks * count((float)more.tiles);
-    }
+    float all = 0.f;
+    each([&](Have h) { all += (float)h.blocks * count((float)h.tiles); });
     return over(all, [](float x) { return wave_sum_f32(x); }, [](float x, float y) { return x + y; }) * p.hkv;
   };
-  float longest = (float)one.tiles;
-  for (int b = tid + kCutThreads; b < p.batch; b += kCutThreads) longest = fmaxf(longest, (float)have(b).tiles);
+  float longest = 0.f;
+  each([&](Have h) { longest = fmaxf(longest, (float)h.tiles); });
   longest = over(longest, [](float x) { return __uint_as_float(~wave_min_u32(~__float_as_uint(x))); }, [](float x, float y) { return fmaxf(x, y); });
   const RowsCost cost = {kRows, c.workers};
   int share = rows_cut(cost, c.least, c.places, false, kMorePieces, longest, sum);
@@ -200,7 +204,7 @@ __global__ __launch_bounds__(kCutThreads) void paged_rows_cut_kernel(RowsCall ca
     int begun = 0;
     for (int b0 = 0; b0 < p.batch; b0 += kCutThreads) {
       const int b = b0 + tid;
-      const Have mine = b0 == 0 ? one : b < p.batch ? have(b) : Have{0, 0};
+      const Have mine = b0 == 0 ? held[0] : b < p.batch ? have(b) : Have{0, 0};
       const int own = p.hkv * mine.blocks * rows_behind(mine.tiles, share, c.places), upto = wave_scan_i32(own, lane);
       if (lane == 63) s_upto[wave] = upto;
       __syncthreads();
