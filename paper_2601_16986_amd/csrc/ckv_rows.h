@@ -18,7 +18,7 @@ CKV_PLAN int turned_by(long long pages, int rows, int group, int n_cu) {
 
 // A workgroup of four wavefronts has 64 or 128 rows (a row is a query head of one of the call's rows), 32 for each of `wide` = 2 or 4 wavefronts side by side; where two do, the others have the other
 // half of the entries.  The entries that they take at once, 32 each, are a tile.  128 rows where there are more than 64: what goes through LDS serves twice as many (us in blocks of 64 and of 128, over 4096 entries
-// of 32 sequences with 8 KV heads, then 777 of 4 with 4: 128 rows 163 and 152, 23.4 and 24.4; 64 rows 106 and 121, 19.7 and 22.2; 32 rows 83 and 101, 18.3 and 21.5).
+// of 32 sequences with 8 KV heads, then 777 of 4 with 4: 8 bits, 128 rows 180 and 174, 24.9 and 23.5; 64 rows 116 and 140, 19.9 and 21.4; 32 rows 90 and 114, 18.4 and 20.4).
 CKV_PLAN int rows_tile(int wide) { return 128 / wide; }
 
 // Which entries a block of rows has to look at, in tiles: those of the first `sinks` entries, and those from the oldest that any row's window holds up to the end of the
@@ -44,9 +44,9 @@ CKV_PLAN u64_t bits_between(long long e0, long long lo, long long hi) {
   return (z >= 64 ? ~0ull : (1ull << z) - 1) & ~((1ull << a) - 1);
 }
 
-// How a call is cut, by what the host knows: every block of rows has `places` places for pieces, of `least` tiles at least (us with 1, 2, 3, 4, 6 tiles of 64 rows, 13 in all: 17.9, 18.5, 20.3, 21.9, -;
-// of 128 rows, 25 in all: -, 23.4, 22.3, 23.8, 24.0).  Up to four pieces for each compute unit, none where there are as many blocks: a piece beside whole blocks costs its beginning, end and joining for nothing
-// (384 blocks of one length 217 us whole, 234 in pieces), but sequences of many lengths leave units idle without (64 drafts of 32 of them 389 whole, 358 in pieces; one sequence of 131072 4360 and 254).
+// How a call is cut, by what the host knows: every block of rows has `places` places for pieces, of `least` tiles at least (us with 1, 3, 4 tiles of 64 rows, 13 in all: 18.6, 20.5, 22.2;
+// with 2, 3, 6, 8 of 128 rows, 25 in all: 23.5, 22.7, 23.7, 26.3).  Up to four pieces for each compute unit, none where there are as many blocks: a piece beside whole blocks costs its beginning, end and joining for nothing
+// (384 blocks of one length 251 us whole, 257 in pieces), but sequences of many lengths leave units idle without (64 drafts of 32 of them 450 whole, 392 in pieces; one sequence of 131072 4940 and 292).
 // Where that could leave one sequence much longer than the others pieces of more than kLongPiece tiles, and a sequence's blocks do not fill the chip by themselves, every block has one place instead, and the pieces behind it,
 // up to kMorePieces for each compute unit, are dealt out by the lengths on the device (paged_rows_cut_kernel).  us, equal places / dealt out: one sequence of 131072 among others of 200, 8 KV heads with 4 each, 2 x 64 drafts 535 / 345,
 // 32 x 64 1780 / 423, 64 x 64 5190 / 412, 64 x 8 1154 / 166, 600 x 8 3350 / 335, parts of 256 rows of 16 5180 / 1087; 32 x 64 of lengths evenly up to 30000 1250 / 1085.  Of one length: 32 x 64 of 8192 585 / 577, 64 x 8 of 2000 92 / 83,

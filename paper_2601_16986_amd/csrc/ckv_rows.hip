@@ -52,7 +52,7 @@ int check_sizes(const ckv_pages* p, const ckv_seqs* s, int rows, int n_q_heads, 
 }
 
 // Whether rows are a token of each sequence, without a tree: bound by memory, the attention of one token takes them (unless they are packed, when some sequence may have none).  By it and as blocks of
-// rows, us: 32 sequences x 8 KV heads x 4 heads, window 4096, 8 bits 55 and 79, bf16 92 and 114; of 16 heads 65 and 79, 100 and 120; one sequence of 131072 54 and 80, 93 and 119; 4 x 4 of 777 9 and 16.
+// rows, us: 32 sequences x 8 KV heads x 4 heads, window 4096, 8 bits 55 and 83, bf16 92 and 116; of 16 heads 66 and 86, 102 and 121; one sequence of 131072 55 and 89, 94 and 119; 4 x 4 of 777 10 and 16.
 bool one_row(const ckv_pages* p, const ckv_seqs* s, int rows, const ckv_mask* m) {
   return rows == 1 && !m->tree && (long long)s->batch * p->n_kv_heads * unit_blocks(s->max_length) <= (1ll << 30);
 }

@@ -156,7 +156,7 @@ __device__ __forceinline__ int even_share(const Paged& p, const RowsAttend& c, i
 }
 
 // The same, once for a call whose blocks may have more pieces than places: cut[0] = tiles of a piece, cut[1 + b] = pieces behind their blocks' places of the sequences before b, numbered by sequence,
-// KV head, block and piece; cut[1 + batch] all of them.  One workgroup, its threads adding up sequences side by side; three trips to memory and a dozen sums over the workgroup.  (Every workgroup of the attention for itself, as
+// KV head, block and piece; cut[1 + batch] all of them.  One workgroup, its threads adding up sequences side by side; three trips to memory and a dozen sums over the workgroup, 5 us.  (Every workgroup of the attention for itself, as
 // without such pieces: 300 sequences of 8 drafts over 500 entries 242 us where they now take 164.)
 constexpr int kCutThreads = 512;
 template <int WIDE>
@@ -228,21 +228,23 @@ __global__ __launch_bounds__(kCutThreads) void paged_rows_cut_kernel(RowsCall ca
 //   outputs  V^T P^T with the logits' registers as operand, entries in the order in which K Q^T leaves them, and values read out of LDS transposed (columns = rows again,
 //            so that what shrinks them is the lane's own too).
 // Weights go in as three bf16 terms, which hold the 24 bits of a float: 32 products for 32 entries where one term would need 16.  (Two terms, 16 bits, take a fifth less time, prompts below 1.44 ms and drafts 245 us where
-// three take 1.79 and 290, and leave outputs that nearly cancel off by up to 2^-17 of their terms: of 8388608 bf16 outputs over up to 9350 entries 20920 then round the other way than the exact ones, 3102 with three
+// three take 1.81 and 290, and leave outputs that nearly cancel off by up to 2^-17 of their terms: of 8388608 bf16 outputs over up to 9350 entries 20920 then round the other way than the exact ones, 3102 with three
 // terms, 7017 in float arithmetic throughout.)  An entry that only some rows of the block see gives the others
 // nothing, whatever its value: where something that is not finite comes out the piece is done again with the finite values alone, and rows that give others weight
 // get NaN where those are.  Where finite values add up to 2^115 it is done once more with lowered weights (lowered_by), whose sums stay finite; the sum of weights, which is not lowered, then has a sign
 // for the join.  No vector register goes to scratch; 67 to
 // 98 scalar ones lie in lanes of vector registers, moved there once (104 to 138, and with 8 bits 16 vector registers in scratch, where the ways that a piece is done again held what they need from the beginning on: 8 drafts of 4
 // short sequences 22.4 us, now 21.4).
-// What bounds it: long pieces of many rows by what moves, in LDS's time and in power: each wavefront reads all keys and values out of LDS for its 32 rows, 16 KB for the 24 products of 32 entries, beside the
-// entries that come in.  A copy that reads nothing out of LDS takes 18 % less, one that loads no entries 18 % less, one without both 28 % (at a higher clock, too), which is what the products take; reads
+// What bounds it: long pieces of many rows by what moves, in LDS's time and in power: each wavefront reads all keys and values out of LDS for its 32 rows, 16 KB for the 32 products of 32 entries, beside the
+// entries that come in.  A copy that reads nothing out of LDS takes 19 % less, one that loads no entries 16 % less, one without both 25 % (at a higher clock, too), which is what the products take; reads
 // asked for a turn earlier change nothing, so it is not their latency; the exponentials and splitting of weights fit between
-// products (3 of them 101 cycles, with all that goes with them 122; two exponentials 29, a pair packed 11, a remainder 8).  Prompts of 2 sequences of 8192, 40 heads, window 4096, bf16 1.43 to 1.58 ms from one card to the next, 1032 GFLOP at 700 TFLOP/s
-// (1050 counting both terms; a large product reaches 1250), no bank of LDS met twice; the clock falls to 2.0 .. 2.2 GHz under it.  8 bits cost the conversion: 48 rows of 40 heads over 131072 entries 230 to 254 us, 540 TFLOP/s.
+// products (3 of them 101 cycles, with all that goes with them 122; two exponentials 29, a pair packed 11, a remainder 8).  Prompts of 2 sequences of 8192, 40 heads, window 4096, bf16 1.80 to 1.88 ms from one card to the next, 1032 GFLOP at 570 TFLOP/s
+// (1140 counting the three terms; a large product reaches 1250), 59 % of cycles in products, no bank of LDS met twice; the clock falls to 1.9 .. 2.0 GHz under it.  8 bits cost the conversion, which every block of rows does for itself, and a quarter
+// of LDS's active cycles are banks met twice as it is written (8.7 M of 35 M): 48 rows of 40 heads over 131072 entries 285 to 310 us, 440 TFLOP/s (890), 48 % of cycles in products; copies without reads, loads and both 13, 16 and 20 % less; parts of
+// prompts of many sequences 41 %, and 9, 11 and 16 % less.
 // Short pieces are bound by what comes one after another: a piece's beginning and end take 30000 cycles (lengths, mask, table, first entries, outputs), a tile of 128 rows by 32 entries 2400 alone and 3700 beside
 // another workgroup.
-// Built, measured and not kept: a step's loads between its products (25 drafts in a window of 1024 55 us instead of 52, prompts no faster), a higher priority for wavefronts that load (the same), 32 rows a workgroup with
+// Built, measured (with two terms) and not kept: a step's loads between its products (25 drafts in a window of 1024 55 us instead of 52, prompts no faster), a higher priority for wavefronts that load (the same), 32 rows a workgroup with
 // 128 entries at once (128 KB of LDS: 8 bits 108 us for 8 rows of 4 heads over 4096 entries of 32 sequences where blocks of 64 rows with idle wavefronts take 83; bf16 113 and 118), 8 bits written to LDS
 // in another order of rows, the next logits a turn early with their largest value beside the last outputs (both the same).
 template <bool E4M3, int WIDE, bool MORE>
